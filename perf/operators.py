@@ -1,0 +1,481 @@
+"""The paged cache's operators: what they are measured on, their plain forms, and their results in 64 bits.
+
+Three kinds of pass, one call of the package each:
+
+* ``append``  a chunk of new tokens for every sequence of a batch: the queries and keys rotated by positions with one
+              to four axes, keys and values written to the pages that each sequence's table names.
+* ``attend``  causal attention of those new tokens (one each, a few, or whole prompts) over the paged rows, with the
+              accumulated attention weights where ``gamma`` is not 0, and scores capped by a tanh where ``cap`` is not.
+* ``evict``   eviction by accumulated weight: every (layer, sequence, KV head) keeps its budget's best rows, the newest
+              and the first ones, and the kept rows beyond the budget move into the places of evicted ones before it.
+
+Head shapes are those of workloads/configs.py (32 query / 8 KV heads of 128, 28 / 4 of 128, 4 / 2 of 64) and a few
+generic ones.  Lengths follow the case alone; contents and page tables the seed.
+"""
+import math
+
+import torch
+
+own = False
+DEV = "cuda"
+
+
+def _case(name, kind, layers, batch, q_heads, kv_heads, dim, page, dtype="bf16", **more):
+    return dict(name=name, kind=kind, layers=layers, batch=batch, q_heads=q_heads, kv_heads=kv_heads, dim=dim, page=page,
+                dtype=dtype, **more)
+
+
+def _append(name, *shape, lo, hi, q_lo, q_hi, axes, rot, adjacent=False, **more):
+    """Cached rows lo .. hi, new tokens q_lo .. q_hi, spread geometrically over the batch."""
+    return _case(name, "append", 1, *shape, lo=lo, hi=hi, q_lo=q_lo, q_hi=q_hi, axes=axes, rot=rot, adjacent=adjacent,
+                 **more)
+
+
+def _attend(name, *shape, lo, hi, q_lo, q_hi, gamma, cap=0.0, long=0, **more):
+    """Rows lo .. hi (the new ones among them), new tokens q_lo .. q_hi; with ``long`` only the last ``long`` sequences
+    have more than one new token."""
+    return _case(name, "attend", 1, *shape, lo=lo, hi=hi, q_lo=q_lo, q_hi=q_hi, gamma=gamma, cap=cap, long=long, **more)
+
+
+def _evict(name, *shape, lo, hi, frac, recent, sink, fresh, **more):
+    """Rows lo .. hi, of which the share ``frac`` stays; the newest ``fresh`` share came after the last eviction."""
+    return _case(name, "evict", *shape, lo=lo, hi=hi, frac=frac, recent=recent, sink=sink, fresh=fresh, **more)
+
+
+def listed():
+    return [
+        # One new token of one user on Llama-8B heads: call and launch latency.
+        _append("append-token", 1, 32, 8, 128, 16, lo=1111, hi=1111, q_lo=1, q_hi=1, axes=1, rot=128),
+        # One token each of a ragged batch of 128, plain text positions, fp16.
+        _append("append-batch128", 128, 32, 8, 128, 64, "f16", lo=100, hi=2000, q_lo=1, q_hi=1, axes=1, rot=128),
+        # Image and video prompts: eight chunks of up to 2048 tokens whose positions have time, height and width.
+        _append("append-video", 8, 32, 8, 128, 64, lo=33, hi=700, q_lo=1500, q_hi=2048, axes=3, rot=128),
+        # Odd chunks of a small model with heads of 64, half of each rotated in adjacent pairs.
+        _append("append-odd", 5, 16, 2, 64, 16, lo=1, hi=300, q_lo=7, q_hi=501, axes=2, rot=32, adjacent=True),
+        # One user's decode step at a short odd length: latency; the scores are kept for the next eviction.
+        _attend("attend-token", 1, 32, 8, 128, 16, lo=1111, hi=1111, q_lo=1, q_hi=1, gamma=0.99),
+        # The ragged batch of 128 on Llama-8B heads, lengths 200 to 12000, one token each.
+        _attend("attend-batch128", 128, 32, 8, 128, 64, lo=200, hi=12000, q_lo=1, q_hi=1, gamma=0.99),
+        # Whole prompts of 2048 tokens, batch 8, whose attention seeds the scores.
+        _attend("attend-prompts", 8, 32, 8, 128, 64, lo=2048, hi=2048, q_lo=2048, q_hi=2048, gamma=1.0),
+        # Chunks of up to 1000 new tokens over 3001 to 12000 rows on Qwen-7B heads, attention alone, capped scores, fp16.
+        _attend("attend-chunks", 4, 28, 4, 128, 16, "f16", lo=3001, hi=12000, q_lo=400, q_hi=1000, gamma=0.0, cap=50.0),
+        # A serving step: 30 users decode while the prompts of two others advance by up to 500 tokens.
+        _attend("attend-mixed", 32, 32, 8, 128, 16, lo=301, hi=5000, q_lo=250, q_hi=500, gamma=1.0, long=2),
+        # One short sequence of one layer: latency.
+        _evict("evict-short", 1, 1, 4, 2, 64, 16, lo=523, hi=523, frac=0.5, recent=32, sink=4, fresh=0.25),
+        # A steady round of the batch-8 workload over its 32 layers: a fifth of the rows goes.
+        _evict("evict-steady", 32, 8, 32, 8, 128, 64, lo=2400, hi=2600, frac=0.8, recent=128, sink=4, fresh=0.2),
+        # A first round after long prompts on Qwen-7B heads: 16384 rows to 30%, eight layers.
+        _evict("evict-long", 8, 16, 28, 4, 128, 64, lo=16384, hi=16384, frac=0.3, recent=256, sink=0, fresh=0.5),
+    ]
+
+
+_HEADS = ((32, 8, 128), (28, 4, 128), (16, 2, 64), (8, 8, 128), (16, 2, 128), (4, 2, 64), (9, 3, 64), (5, 1, 128))
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    while True:
+        kind = rng.choice(("append", "attend", "attend", "evict"))
+        hq, hk, d = rng.choice(_HEADS)
+        batch = _log(rng, 1, 128)
+        shape = (hq, hk, d, rng.choice((16, 32, 64, 128)), rng.choice(("bf16", "bf16", "f16")))
+        if kind == "append":
+            lo, q_lo = _log(rng, 1, 3000), _log(rng, 1, 1500)
+            axes = rng.choice((1, 1, 2, 3, 4))
+            c = _append("", batch, *shape, lo=lo, hi=_log(rng, lo, 3 * lo), q_lo=q_lo, q_hi=_log(rng, q_lo, 2 * q_lo),
+                        axes=axes, rot=rng.choice((d, d, d // 2)), adjacent=rng.random() < 0.3)
+            most = 0.8e9
+        elif kind == "attend":
+            form = rng.choice(("token", "token", "chunk", "mixed"))
+            lo = _log(rng, 60, 12000)
+            hi = _log(rng, lo, 4 * lo)
+            q_lo, q_hi, long = 1, 1, 0
+            if form != "token":
+                q_lo = _log(rng, 2, min(lo, 1500))
+                q_hi = _log(rng, q_lo, min(lo, 2 * q_lo))
+                long = rng.randint(1, batch) if form == "mixed" else 0
+            c = _attend("", batch, *shape, lo=lo, hi=hi, q_lo=q_lo, q_hi=q_hi, gamma=rng.choice((0.0, 0.9, 0.99, 1.0)),
+                        cap=rng.choice((0.0, 0.0, 30.0, 50.0)), long=long)
+            most = 3.5e9
+        else:
+            lo = _log(rng, 100, 16000)
+            c = _evict("", _log(rng, 1, 32), batch, *shape, lo=lo, hi=min(24000, _log(rng, lo, 2 * lo)),
+                       frac=rng.choice((0.3, 0.5, 0.8, 0.95)), recent=rng.choice((0, 32, 64, 256)),
+                       sink=rng.choice((0, 0, 4)), fresh=rng.choice((0.02, 0.1, 0.25, 0.5)))
+            most = 2e9
+        del c["name"]
+        w, geo = work(c), _Geometry(c)
+        pool = geo.pages * c["kv_heads"] * c["page"] * c["dim"] * 4
+        # The plain form holds every new token's scores over every row of the longest sequence.
+        grid = 4.0 * c["batch"] * c["q_heads"] * geo.max_q * geo.max_kv if kind == "attend" else 0.0
+        wide = 4.0 * c["batch"] * c["kv_heads"] * c["dim"] * geo.max_kv if kind == "attend" else 0.0
+        if w["bytes"] <= most and w["flops"] <= 2.8e11 and pool <= 5e9 and grid <= 1.3e10 and wide <= 1e10:
+            return c
+
+
+class _Geometry:
+    """Rows and new tokens of every sequence, and the pages that they take (the seed plays no part)."""
+
+    def __init__(self, c):
+        B, ps = c["batch"], c["page"]
+        step = next(s for s in (7, 5, 3, 2, 1) if math.gcd(s, B) == 1)
+        quant = [(step * b % B + 0.5) / B for b in range(B)]
+        spread = lambda lo, hi: [int(lo * (hi / lo) ** x) for x in quant]  # noqa: E731
+        self.n = spread(c["lo"], c["hi"])
+        self.q = spread(c["q_lo"], c["q_hi"]) if "q_lo" in c else [0] * B
+        if c.get("long"):
+            self.q = [q if b >= B - c["long"] else 1 for b, q in enumerate(self.q)]
+        self.q_start = [sum(self.q[:b]) for b in range(B)]
+        self.rows = sum(self.q)
+        self.max_q, self.max_kv = max(self.q), max(self.n)
+        room = [n + q if c["kind"] == "append" else n for n, q in zip(self.n, self.q)]
+        self.used = [-(-r // ps) for r in room]  # pages of a sequence in one layer
+        self.table = max(self.used) + 1
+        self.pages = c["layers"] * sum(self.used) + 3
+
+
+def _dtype(c):
+    return torch.float16 if c["dtype"] == "f16" else torch.bfloat16
+
+
+def _sections(c):
+    """Pairs of each axis: the first axis of several has the fewest, as the time axis of video positions."""
+    pairs, A = c["rot"] // 2, c["axes"]
+    if A == 1:
+        return [pairs]
+    first = pairs // (A + 1)
+    rest = [(pairs - first) // (A - 1)] * (A - 1)
+    rest[-1] += pairs - first - sum(rest)
+    return [first] + rest
+
+
+def prepare(case, seed):
+    c = case
+    geo = _Geometry(c)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed * 7919 + 17)
+    Ly, B, HQ, HK, D, ps, dt = c["layers"], c["batch"], c["q_heads"], c["kv_heads"], c["dim"], c["page"], _dtype(c)
+    rand = lambda *s: torch.rand(s, generator=g, device=DEV)  # noqa: E731
+    randn = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    ints = lambda v, t=torch.int32: torch.tensor(v, dtype=t, device=DEV)  # noqa: E731
+    P = geo.pages
+    # Keys with a Zipf-like weight along one direction a head, which the queries look for; values N(0, 1).
+    u = randn(HK, D)
+    u = u / u.norm(dim=-1, keepdim=True)
+    k = torch.empty((P, HK, ps, D), dtype=dt, device=DEV).normal_(generator=g)
+    v = torch.empty((P, HK, ps, D), dtype=dt, device=DEV).normal_(generator=g)
+    beta = -torch.log(1.0 + torch.floor(rand(P, HK, ps) * geo.max_kv))
+    for p0 in range(0, P, 4096):
+        k[p0:p0 + 4096] += (beta[p0:p0 + 4096, :, :, None] * u[None, :, None, :]).to(dt)
+    # pos, score and the lengths share one buffer, so that one copy brings all of them back before a pass.
+    rows = P * HK * ps
+    meta = torch.empty(2 * rows + 2 * Ly * B, dtype=torch.int32, device=DEV)
+    pos, score = meta[:rows].view(P, HK, ps), meta[rows:2 * rows].view(torch.float32).view(P, HK, ps)
+    lens, seen = meta[2 * rows:2 * rows + Ly * B].view(Ly, B), meta[2 * rows + Ly * B:].view(Ly, B)
+    score.copy_(torch.exp(1.2 * beta + 0.5 * randn(P, HK, ps)) * (rand(P, HK, ps) > 0.02))
+    lens.copy_(ints([geo.n] * Ly))
+    seen.copy_(lens)
+    # Pages in no order; the entries past a sequence's rows name no page.
+    ids = torch.randperm(P, generator=g, device=DEV).int()
+    table = torch.full((Ly, B, geo.table), -1, dtype=torch.int32, device=DEV)
+    used = torch.arange(geo.table, device=DEV)[None, None, :] < ints(geo.used)[None, :, None]
+    used = used.expand(Ly, B, geo.table)
+    table[used] = ids[:int(used.sum())]
+    s = {"case": c, "k": k, "v": v, "score": score, "pos": pos, "len": lens, "seen": seen, "table": table, "meta": meta}
+    if c["kind"] == "evict":
+        n = ints([geo.n] * Ly)[:, :, None, None]
+        old = n - (n.float() * c["fresh"]).int()
+        r = torch.arange(geo.max_kv, device=DEV)[None, None, None, :]
+        # What the last eviction left: tokens in any order, the first sixteen among them; then those since, in order.
+        order = torch.where(r < old, rand(Ly, B, HK, geo.max_kv), 2.0).argsort(dim=-1).argsort(dim=-1).int()
+        gaps = torch.where(order < 16, order, 2 * order - 16 + (rand(Ly, B, HK, geo.max_kv) < 0.5).int())
+        p = torch.where(r < old, gaps, 2 * old + r - old)
+        at = _rows(s, geo.max_kv)
+        live = (r < n).expand(at.shape)
+        pos.zero_()
+        pos.view(-1)[at[live]] = p.expand(at.shape)[live].int()
+        seen.copy_((n + old)[:, :, 0, 0])
+        s["budget"] = (lens.float() * c["frac"]).int().t().contiguous()
+    else:
+        s["q_start"], s["q_len"] = ints(geo.q_start, torch.int64), ints(geo.q)
+        s["max_q"], s["max_kv"], s["rows"] = geo.max_q, geo.max_kv, geo.rows
+        ar = torch.arange(P * ps, device=DEV, dtype=torch.int32).view(P, 1, ps)
+        pos.copy_(ar.expand(P, HK, ps))
+    if c["kind"] == "append":
+        # One projection's packed output: queries, keys and values of a token side by side.
+        qkv = randn(geo.rows, (HQ + 2 * HK) * D).to(dt)
+        s["q"], s["k_new"], s["v_new"] = (x.view(geo.rows, -1, D) for x in qkv.split((HQ * D, HK * D, HK * D), dim=1))
+        first = torch.cat([torch.arange(n, n + q) for n, q in zip(geo.n, geo.q)]).to(DEV)
+        axis = torch.stack([first.int() if a == 0 else (rand(geo.rows) * 200).int() for a in range(c["axes"])])
+        s["axis_pos"] = axis.contiguous()
+        s["inv_freq"] = (500000.0 ** (-torch.arange(0, c["rot"], 2, device=DEV, dtype=torch.float64) / c["rot"])).float()
+        s["sections"] = _sections(c)
+        s["q_out"] = torch.zeros((geo.rows, HQ, D), dtype=dt, device=DEV)
+    if c["kind"] == "attend":
+        s["q"] = (randn(geo.rows, HQ, D) + 5.0 * u.repeat_interleave(HQ // HK, dim=0)).to(dt)
+        s["out"] = torch.zeros((geo.rows, HQ, D), dtype=dt, device=DEV)
+    s["meta0"] = meta.clone()
+    if own:
+        from paper_2511_06029_amd import lethe as L
+        s["L"] = L
+        s["cache"] = cache = L.LethePagedCache(k, v, score, pos, lens, seen, table, HQ)
+        if c["kind"] == "append":
+            s["rotary"] = L.Rotary(s["inv_freq"], s["axis_pos"], s["sections"], adjacent=c["adjacent"])
+        if c["kind"] == "attend":
+            s["ws"] = cache.attn_workspace(geo.rows, geo.max_q, geo.max_kv)
+        if c["kind"] == "evict":
+            s["ws"] = cache.evict_workspace()
+    return s
+
+
+def _rows(s, N):
+    """Where row r < N of every (layer, sequence, KV head) lies in the pools seen as rows: [layers][batch][heads][N].
+    Rows past the table's pages are given some place."""
+    P, HK, ps, _ = s["k"].shape
+    r = torch.arange(N, device=DEV)
+    page = s["table"].long()[:, :, (r // ps).clamp(max=s["table"].shape[2] - 1)].clamp(min=0)
+    heads = torch.arange(HK, device=DEV)
+    return ((page[:, :, None, :] * HK + heads[None, None, :, None]) * ps) + (r % ps)
+
+
+def _tokens(s):
+    """The sequence of every new token and its place among the sequence's new ones."""
+    ql = s["q_len"].long()
+    b = torch.repeat_interleave(torch.arange(len(ql), device=DEV), ql, output_size=s["rows"])
+    return b, torch.arange(s["rows"], device=DEV) - s["q_start"][b]
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Plain forms: 32 bits, rounded once at the end
+# ---------------------------------------------------------------------------------------------------------------------
+def _plain_append(s):
+    c = s["case"]
+    rot, D, HK, ps = c["rot"], c["dim"], c["kv_heads"], c["page"]
+    half = rot // 2
+    axis = torch.repeat_interleave(torch.arange(c["axes"], device=DEV), torch.tensor(s["sections"], device=DEV),
+                                   output_size=half)
+    angle = s["axis_pos"].double()[axis].t() * s["inv_freq"].double()
+    cos, sin = angle.cos().float()[:, None, :], angle.sin().float()[:, None, :]
+
+    def turn(x):
+        x = x.float()
+        y = x.clone()
+        if c["adjacent"]:
+            a, b = x[..., 0:rot:2], x[..., 1:rot:2]
+            y[..., 0:rot:2], y[..., 1:rot:2] = a * cos - b * sin, b * cos + a * sin
+        else:
+            a, b = x[..., :half], x[..., half:rot]
+            y[..., :half], y[..., half:rot] = a * cos - b * sin, b * cos + a * sin
+        return y.to(s["k"].dtype)
+
+    s["q_out"].copy_(turn(s["q"]))
+    b, i = _tokens(s)
+    row = s["len"][0].long()[b] + i
+    page = s["table"][0].long()[b, row // ps]
+    at = (page[:, None] * HK + torch.arange(HK, device=DEV)) * ps + (row % ps)[:, None]
+    s["k"].view(-1, D)[at] = turn(s["k_new"])
+    s["v"].view(-1, D)[at] = s["v_new"].contiguous()
+    s["score"].view(-1)[at] = 0.0
+    s["pos"].view(-1)[at] = (s["seen"][0].long()[b] + i).int()[:, None].expand(-1, HK).contiguous()
+    s["len"][0] += s["q_len"]
+    s["seen"][0] += s["q_len"]
+
+
+def _plain_attend(s):
+    c = s["case"]
+    B, HQ, HK, D = c["batch"], c["q_heads"], c["kv_heads"], c["dim"]
+    G, N, Q = HQ // HK, s["max_kv"], s["max_q"]
+    at = _rows(s, N)[0]
+    n, ql = s["len"][0].long(), s["q_len"].long()
+    K, V = s["k"].view(-1, D)[at].float(), s["v"].view(-1, D)[at].float()
+    i = torch.arange(Q, device=DEV)
+    src = (s["q_start"][:, None] + i[None, :].clamp(max=Q)).clamp(max=s["rows"] - 1)
+    q = s["q"][src].float().view(B, Q, HK, G, D).permute(0, 2, 3, 1, 4).reshape(B, HK, G * Q, D)
+    x = torch.matmul(q, K.transpose(2, 3)) / math.sqrt(D)
+    if c["cap"]:
+        x = c["cap"] * torch.tanh(x / c["cap"])
+    r = torch.arange(N, device=DEV)
+    hidden = r[None, None, :] > (n - ql)[:, None, None] + i[None, :, None]
+    hidden = hidden | (i[None, :, None] >= ql[:, None, None])
+    x = x.view(B, HK, G, Q, N).masked_fill_(hidden[:, None, None], -math.inf)
+    x = torch.exp(x - x.amax(dim=-1, keepdim=True).clamp(min=-1e30))
+    x /= x.sum(dim=-1, keepdim=True).clamp(min=1e-30)
+    out = torch.matmul(x.view(B, HK, G * Q, N), V).view(B, HK, G, Q, D).permute(0, 3, 1, 2, 4).reshape(B, Q, HQ, D)
+    b, j = _tokens(s)
+    s["out"].copy_(out[b, j])
+    if c["gamma"]:
+        live = (r[None, None, :] < n[:, None, None]).expand(B, HK, N)
+        new = c["gamma"] * s["score"].view(-1)[at] + x.sum(dim=(2, 3))
+        s["score"].view(-1)[at[live]] = new[live]
+
+
+def _kept(s, N, score, pos, live):
+    """The rows of every segment that stay (all of them, where the budget has room)."""
+    c = s["case"]
+    n, k = s["len"].long()[:, :, None, None], s["budget"].long().t()[:, :, None, None].clamp(min=0)
+    new = k.clamp(max=c["recent"])
+    first = (k - new).clamp(max=c["sink"])
+    age = torch.where(live, pos.long(), 1 << 40).argsort(dim=-1).argsort(dim=-1)  # 0: the oldest token
+    held = live & ((age < first) | (age >= n - new))
+    # Scores as whole numbers in the same order, the older token first among equals.
+    bits = (score + 0.0).view(torch.int32).long()
+    bits = torch.where(bits < 0, -(bits & 0x7FFFFFFF), bits)
+    bits = torch.where(score.isnan(), -(1 << 32), bits)
+    rank = torch.where(live & ~held, bits * (1 << 20) - age, -(1 << 62)).argsort(dim=-1, descending=True).argsort(dim=-1)
+    return (held | (live & ~held & (rank < k - new - first)) | (live & (n <= k))), k
+
+
+def _plain_evict(s):
+    c = s["case"]
+    D, N = c["dim"], int(s["table"].shape[2] * c["page"])
+    at = _rows(s, N)
+    r = torch.arange(N, device=DEV)
+    live = (r < s["len"].long()[:, :, None, None]).expand(at.shape)
+    keep, k = _kept(s, N, s["score"].view(-1)[at], s["pos"].view(-1)[at], live)
+    # The i-th kept row from the budget on goes to the place of the i-th evicted row before it.
+    dst, src = at[live & ~keep & (r < k)], at[keep & (r >= k) & (s["len"].long()[:, :, None, None] > k)]
+    for x in (s["k"].view(-1, D), s["v"].view(-1, D), s["score"].view(-1), s["pos"].view(-1)):
+        x[dst] = x[src]
+    s["len"].copy_(torch.minimum(s["len"], k[:, :, 0, 0].int()))
+
+
+def run(state):
+    s, c = state, state["case"]
+    kind = c["kind"]
+    if kind == "append":
+        s["len"].copy_(s["meta0"][-2 * c["batch"]:-c["batch"]].view(1, -1))
+        s["seen"].copy_(s["meta0"][-c["batch"]:].view(1, -1))
+        if own:
+            s["L"].paged_append(s["cache"], 0, s["q"], s["k_new"], s["v_new"], s["q_start"], s["q_len"], s["rotary"],
+                                s["q_out"])
+        else:
+            _plain_append(s)
+        return {x: s[x] for x in ("q_out", "k", "v", "pos", "score", "len", "seen")}
+    if kind == "attend":
+        if own:
+            s["L"].paged_attn_score(s["cache"], 0, s["q"], s["q_start"], s["q_len"], s["max_q"], s["max_kv"],
+                                    c["gamma"], 0.0, c["cap"], s["out"], s["ws"])
+        else:
+            _plain_attend(s)
+        return {"out": s["out"], "score": s["score"]} if c["gamma"] else {"out": s["out"]}
+    # The rounds of a serving loop find new scores and lengths each time; here the same ones come back.
+    s["meta"].copy_(s["meta0"])
+    if own:
+        s["L"].paged_evict(s["cache"], s["budget"], c["recent"], c["sink"], s["ws"])
+    else:
+        _plain_evict(s)
+    return {x: s[x] for x in ("k", "v", "score", "pos", "len")}
+
+
+def work(case):
+    c = case
+    geo = _Geometry(c)
+    HQ, HK, D = c["q_heads"], c["kv_heads"], c["dim"]
+    if c["kind"] == "append":
+        return {"bytes": geo.rows * ((HQ + 2 * HK) * D * 4 + HK * 8 + 4 * c["axes"]), "flops": geo.rows * (HQ + HK) * c["rot"] * 3}
+    if c["kind"] == "attend":
+        rows = HK * sum(geo.n)
+        pairs = sum(q * (n - q) + q * (q + 1) / 2 for q, n in zip(geo.q, geo.n))
+        byt = rows * (4 * D + (8 if c["gamma"] else 0)) + geo.rows * HQ * D * 4
+        return {"bytes": byt, "flops": 4.0 * D * HQ * pairs}
+    rows = moved = 0
+    for n in geo.n:
+        k = int(n * c["frac"])
+        new, first = min(c["recent"], k), min(c["sink"], max(k - c["recent"], 0))
+        share = (k - new - first) / max(n - new - first, 1)  # of the rows that are not held
+        rows += n
+        moved += (k - first) * (1.0 - share) if k < n else 0  # the evicted ones before the budget
+    seg = c["layers"] * HK
+    return {"bytes": seg * (8.0 * rows + moved * 2 * (4 * D + 8)), "flops": 0.0}
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# 64 bits, one sequence at a time
+# ---------------------------------------------------------------------------------------------------------------------
+def exact(case, seed):
+    global own
+    c, was = case, own
+    own = False
+    s = prepare(c, seed)
+    own = was
+    geo = _Geometry(c)
+    HQ, HK, D, ps = c["q_heads"], c["kv_heads"], c["dim"], c["page"]
+    G = HQ // HK
+    table = s["table"].cpu().tolist()
+
+    def slots(l, b, r0, r1):
+        """[heads][rows] places of rows r0 .. r1 in the pools seen as rows."""
+        page = torch.tensor([table[l][b][r // ps] for r in range(r0, r1)], device=DEV)
+        off = torch.arange(r0, r1, device=DEV) % ps
+        return torch.stack([(page * HK + h) * ps + off for h in range(HK)])
+
+    if c["kind"] == "append":
+        if geo.pages * HK * ps * D > 4e8:
+            return None
+        k, v, score, q_out = s["k"].double(), s["v"].double(), s["score"].double(), s["q"].double().clone()
+        first, spans = 0, []
+        for a, m in enumerate(s["sections"]):
+            spans += [(a, j) for j in range(first, first + m)]
+            first += m
+        half, k_new = c["rot"] // 2, s["k_new"].double().clone()
+        for a, j in spans:
+            i0, i1 = (2 * j, 2 * j + 1) if c["adjacent"] else (j, j + half)
+            z = torch.polar(torch.ones(geo.rows, dtype=torch.float64, device=DEV),
+                            s["axis_pos"][a].double() * s["inv_freq"][j].double())[:, None]
+            for x in (q_out, k_new):
+                w = torch.complex(x[:, :, i0].clone(), x[:, :, i1].clone()) * z
+                x[:, :, i0], x[:, :, i1] = w.real, w.imag
+        for b in range(c["batch"]):
+            at = slots(0, b, geo.n[b], geo.n[b] + geo.q[b])
+            new = slice(geo.q_start[b], geo.q_start[b] + geo.q[b])
+            k.view(-1, D)[at] = k_new[new].transpose(0, 1).contiguous()
+            v.view(-1, D)[at] = s["v_new"][new].double().transpose(0, 1).contiguous()
+            score.view(-1)[at] = 0.0
+        return {"q_out": q_out, "k": k, "v": v, "pos": None, "score": score, "len": None, "seen": None}
+    if c["kind"] == "attend":
+        out = torch.zeros(s["out"].shape, dtype=torch.float64, device=DEV)
+        score = s["score"].double()
+        for b in range(c["batch"]):
+            n, m, q0 = geo.n[b], geo.q[b], geo.q_start[b]
+            at = slots(0, b, 0, n)
+            hidden = torch.ones((m, n), dtype=torch.bool, device=DEV).triu(n - m + 1)
+            for h in range(HK):
+                K, V = s["k"].view(-1, D)[at[h]].double(), s["v"].view(-1, D)[at[h]].double()
+                total = torch.zeros(n, dtype=torch.float64, device=DEV)
+                for i in range(h * G, (h + 1) * G):
+                    x = torch.mm(s["q"][q0:q0 + m, i].double(), K.t().contiguous()) * D ** -0.5
+                    if c["cap"]:
+                        x = torch.tanh(x / c["cap"]) * c["cap"]
+                    p = torch.softmax(x.masked_fill_(hidden, -math.inf), dim=1)
+                    out[q0:q0 + m, i] = torch.mm(p, V)
+                    total += p.sum(0)
+                if c["gamma"]:
+                    score.view(-1)[at[h]] = c["gamma"] * score.view(-1)[at[h]] + total
+        return {"out": out, "score": score} if c["gamma"] else {"out": out}
+    if c["layers"] * c["batch"] * HK > 600:
+        return None
+    score, pos = s["score"].view(-1).cpu(), s["pos"].view(-1).cpu()
+    place = torch.arange(score.numel())  # which row lies at each place afterwards
+    for l in range(c["layers"]):
+        for b in range(c["batch"]):
+            n, k = geo.n[b], int(s["budget"][b, l])
+            if k >= n:
+                continue
+            new, first = min(c["recent"], k), min(c["sink"], max(k - c["recent"], 0))
+            for at in slots(l, b, 0, n).cpu():
+                by_age = torch.argsort(pos[at])
+                held = torch.cat([by_age[:first], by_age[n - new:]])
+                rest = by_age[first:n - new]
+                best = rest[torch.sort(score[at[rest]].double(), descending=True, stable=True).indices[:k - new - first]]
+                stays = torch.zeros(n, dtype=torch.bool)
+                stays[torch.cat([held, best])] = True
+                place[at[:k][~stays[:k]]] = at[k:][stays[k:]]
+    place = place.to(DEV)
+    return {"k": s["k"].view(-1, D)[place].view(s["k"].shape).double(),
+            "v": s["v"].view(-1, D)[place].view(s["v"].shape).double(),
+            "score": s["score"].view(-1)[place].view(s["score"].shape).double(), "pos": None, "len": None}
