@@ -351,8 +351,8 @@ def run(state):
         s["len"].copy_(s["meta0"][-2 * c["batch"]:-c["batch"]].view(1, -1))
         s["seen"].copy_(s["meta0"][-c["batch"]:].view(1, -1))
         if own:
-            s["L"].paged_append(s["cache"], 0, s["q"], s["k_new"], s["v_new"], s["q_start"], s["q_len"], s["rotary"],
-                                s["q_out"])
+            s["L"].paged_append(s["cache"], 0, s["q"], s["k_new"], s["v_new"], s["q_start"], s["q_len"], s["max_q"],
+                                s["rotary"], s["q_out"])
         else:
             _plain_append(s)
         return {x: s[x] for x in ("q_out", "k", "v", "pos", "score", "len", "seen")}
