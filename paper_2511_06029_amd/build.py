@@ -25,7 +25,7 @@ FILE_FLAGS = {"compact.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip"))) + [os.path.join(CSRC, "lethe_api.cpp")]
+    return sorted(glob.glob(os.path.join(CSRC, "*.hip"))) + sorted(glob.glob(os.path.join(CSRC, "*.cpp")))
 
 
 def build(verbose=False):
