@@ -67,7 +67,8 @@ typedef enum {
   LETHE_ERR_HIP = -4          /* the HIP runtime rejected a launch                 */
 } lethe_status;
 
-typedef enum { LETHE_BF16 = 0, LETHE_F32 = 1 } lethe_dtype;
+/* LETHE_F16 is a type of paged caches only (lethe_paged_cache below). */
+typedef enum { LETHE_BF16 = 0, LETHE_F32 = 1, LETHE_F16 = 2 } lethe_dtype;
 
 /* Bits OR-ed into *dev_status by the kernels. */
 #define LETHE_DEV_APPEND_OVERFLOW 1 /* append with len == cap: sequence skipped      */
@@ -479,6 +480,179 @@ lethe_status lethe_decode_attn_score_compact(const lethe_cache* cache, int32_t l
  * LETHE_ERR_UNSUPPORTED, LETHE_ERR_HIP.
  */
 lethe_status lethe_score_flush(const lethe_cache* cache, hipStream_t stream);
+
+/*
+ * Paged cache
+ * -----------
+ * The same hot path over a cache in pages: a pool of pages shared by every
+ * layer and sequence, so that what eviction frees in one layer serves another
+ * layer or a new sequence.  Three calls work on it: lethe_paged_append (rotate
+ * and write new tokens), lethe_paged_attn_score (their attention, one token
+ * or a chunk a sequence) and lethe_paged_evict (bring every segment to its
+ * budget).
+ *
+ *  A page holds page_size rows of every KV head.  Row r of (layer l, sequence
+ *  b, KV head h) is row r % page_size of head h in page
+ *      page_table[(l * num_seqs + b) * max_pages + r / page_size],
+ *  for r < len[l * num_seqs + b].  Table entries past the last live row are
+ *  not read.  A page belongs to one (layer, sequence), except that calls that
+ *  only read it (attention with gamma 0) may find it in several tables.
+ *  Rows of a segment are in no particular order (eviction moves them): pos
+ *  holds each row's token, counted from 0 in the order of appending, and
+ *  seen[l * num_seqs + b] the number of tokens ever appended.  The caller
+ *  starts len and seen at 0 and owns the page table; the calls read it only.
+ *
+ *  Conventions are those above (caller-owned device memory, asynchronous on
+ *  `stream`, dev_status bits, no allocation, no state between calls).  k, v,
+ *  and the q / k_new / v_new / q_out / out arguments (NULL with q_rows 0 is
+ *  fine) must be 16-byte aligned, workspaces 256-byte aligned.
+ *  A page number outside [0, num_pages) sets LETHE_DEV_BAD_LAYOUT; what else
+ *  it does is said at each call.  Sums are in a fixed order: the same call on
+ *  the same inputs gives the same bits.
+ */
+typedef struct {
+  void* k;                    /* dtype [num_pages][num_kv_heads][page_size][head_dim]        */
+  void* v;                    /* dtype [num_pages][num_kv_heads][page_size][head_dim]        */
+  float* score;               /* fp32  [num_pages][num_kv_heads][page_size]                  */
+  int32_t* pos;               /* int32 [num_pages][num_kv_heads][page_size] token of the row */
+  int32_t* len;               /* int32 [num_layers][num_seqs] live rows                      */
+  int32_t* seen;              /* int32 [num_layers][num_seqs] tokens appended so far         */
+  const int32_t* page_table;  /* int32 [num_layers][num_seqs][max_pages]                     */
+  int64_t num_pages;          /* num_pages * num_kv_heads * page_size < 2^31                 */
+  int32_t page_size;          /* a power of two, 16 .. 1024                                  */
+  int32_t max_pages;          /* max_pages * page_size < 2^31                                */
+  int32_t num_layers;         /* 1 .. 256                                                    */
+  int32_t num_seqs;           /* 1 .. 1024                                                   */
+  int32_t num_q_heads;
+  int32_t num_kv_heads;       /* num_q_heads / num_kv_heads in 1 .. 8                        */
+  int32_t head_dim;           /* 64 or 128                                                   */
+  lethe_dtype dtype;          /* LETHE_BF16 or LETHE_F16 (LETHE_F32 is unsupported)          */
+  int32_t* dev_status;        /* int32 [1], LETHE_DEV_* bits                                 */
+} lethe_paged_cache;
+
+#define LETHE_MAX_AXES 4
+
+/*
+ * Rotary positions with one to four axes (text: one; images and video: time,
+ * height, width).  Pair j < rot_dim / 2 of a head belongs to the axis whose
+ * section holds it (the first sections[0] pairs to axis 0, the next
+ * sections[1] to axis 1, ...) and turns by
+ *     theta = axis_pos[axis][row] * inv_freq[j]
+ * as (x, y) -> (x cos theta - y sin theta, y cos theta + x sin theta), where
+ * (x, y) are elements j and j + rot_dim / 2 of the head, or, with adjacent,
+ * elements 2 j and 2 j + 1.  Elements from rot_dim on stay.  theta is formed
+ * in 64 bits, so far positions keep their angle.
+ */
+typedef struct {
+  const float* inv_freq;    /* fp32 [rot_dim / 2] (device)                        */
+  const int32_t* axis_pos;  /* int32 [num_axes][q_rows] (device), any sign        */
+  int32_t rot_dim;          /* a multiple of 16, 16 .. head_dim                   */
+  int32_t num_axes;         /* 1 .. LETHE_MAX_AXES                                */
+  int32_t sections[LETHE_MAX_AXES]; /* pairs of each axis, >= 0, rot_dim / 2 in all */
+  int32_t adjacent;         /* 0: pairs (j, j + rot_dim / 2); 1: pairs (2 j, 2 j + 1) */
+} lethe_rotary;
+
+/*
+ * Append new tokens to layer `layer`.  Sequence b comes with q_len[b] >= 0
+ * tokens, rows q_start[b] .. q_start[b] + q_len[b] - 1 of q, k_new and v_new
+ * (rows of different sequences do not overlap; rows of none are left alone,
+ * in q_out too).  Token i of sequence b
+ *   - becomes row len + i of every KV head: k_new rotated, v_new as it is,
+ *     score 0, pos = seen + i;
+ *   - has its queries rotated into q_out (not with q NULL).
+ * Then len and seen grow by q_len.  rotary NULL rotates nothing.
+ *
+ *  q      dtype [q_rows][num_q_heads][head_dim], rows q_stride elements apart;
+ *         NULL exactly when q_out is.  k_new, v_new dtype
+ *         [q_rows][num_kv_heads][head_dim], rows k_stride and v_stride apart:
+ *         the three may be parts of one packed projection.  Strides are
+ *         multiples of 8 and at least a row.
+ *  q_out  dtype [q_rows][num_q_heads][head_dim], contiguous; may be q itself
+ *         where q is contiguous.
+ *  q_start int64 [num_seqs], q_len int32 [num_seqs] (device); max_q_len host
+ *         upper bound of q_len[b].
+ * A sequence whose rows would not fit its table sets
+ * LETHE_DEV_APPEND_OVERFLOW; one with a page out of range among those it
+ * would write, sizes that do not fit together or seen beyond 2^31 sets
+ * LETHE_DEV_BAD_LAYOUT.  Nothing of such a sequence is appended (its q_out
+ * rows are written where its rows lie within q_rows).  Errors:
+ * LETHE_ERR_INVALID, LETHE_ERR_UNSUPPORTED, LETHE_ERR_HIP.
+ */
+lethe_status lethe_paged_append(const lethe_paged_cache* cache, int32_t layer, const void* q, int64_t q_stride,
+                                const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                                const int64_t* q_start, const int32_t* q_len, int64_t q_rows, int32_t max_q_len,
+                                const lethe_rotary* rotary, void* q_out, hipStream_t stream);
+
+/*
+ * Attention of the newest rows of layer `layer` over the paged rows, for a
+ * batch that may mix decode steps (one query), a few queries and chunks of a
+ * prompt.  The q_len[b] newest of a sequence's n = len rows come with queries
+ * (their K and V appended before); query i attends rows 0 .. n - q_len[b] + i.
+ * For query head j = h G + g:
+ *     x = softmax_scale * q[row][j][:] . K[r][:]
+ *     x = softcap * tanh(x / softcap)                     (softcap > 0 only)
+ *     P = softmax(x),  out[row][j][:] = sum_r P_r V[r][:]
+ * and, with gamma > 0, for every row r < n of a sequence with q_len[b] > 0:
+ *     s_r <- gamma * s_r + sum_{g < G} sum_i P_{hG+g, i, r}
+ * (for one query a sequence this is Eq. 5; the update is applied within the
+ * call).  gamma 0 leaves the scores alone, and cache->score may be NULL.
+ *
+ *  q, out   dtype [q_rows][num_q_heads][head_dim]; out is the result rounded
+ *           once to dtype (sums and statistics are fp32, the weights of the
+ *           P V product are rounded to dtype).  Rows of no sequence are left
+ *           alone.
+ *  q_start, q_len, q_rows, max_q_len, max_kv_len  as for
+ *           lethe_prefill_attn_score; the bounds choose the kernels and size
+ *           the workspace.  Row ranges must not overlap.
+ *  softmax_scale  > 0, or <= 0 for 1/sqrt(head_dim); softcap >= 0, 0 for none.
+ *  ws       lethe_paged_attn_workspace_bytes(cache, q_rows, max_q_len,
+ *           max_kv_len) bytes, not shared by calls that may run at once.
+ * A row on a page out of range is not attended and its score not updated; a
+ * query that is left with no row gets 0.  A sequence whose sizes do not fit
+ * (q_len < 0 or > len, a bound exceeded, rows outside [0, q_rows)) sets
+ * LETHE_DEV_BAD_LAYOUT and is left alone.  What lies in rows that a query does
+ * not attend never reaches its output, infinities and NaN included.  Errors:
+ * LETHE_ERR_INVALID, LETHE_ERR_UNSUPPORTED, LETHE_ERR_WORKSPACE,
+ * LETHE_ERR_HIP.
+ */
+lethe_status lethe_paged_attn_score(const lethe_paged_cache* cache, int32_t layer, const void* q,
+                                    const int64_t* q_start, const int32_t* q_len, int64_t q_rows, int32_t max_q_len,
+                                    int32_t max_kv_len, float gamma, float softmax_scale, float softcap, void* out,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of such a call; 0 for an invalid description or bounds. */
+size_t lethe_paged_attn_workspace_bytes(const lethe_paged_cache* cache, int64_t q_rows, int32_t max_q_len,
+                                        int32_t max_kv_len);
+
+/*
+ * Eviction by accumulated weight, for every segment (l, b, h) with n live
+ * rows and budget k = max(budget[b][l], 0):
+ *   k >= n: nothing.  Otherwise r = min(recent, k), s = min(sink, k - r); the
+ *   r rows of the newest tokens stay, the s rows of the oldest, and of the
+ *   others the first k - r - s in the order (score descending, token
+ *   ascending), where +0 and -0 tie and NaN ranks after every number: the
+ *   rule of lethe_rasr_select, with tokens for rows.
+ *   The i-th kept row at or after row k (in row order) then moves, bit for
+ *   bit with its score and pos, into the place of the i-th evicted row before
+ *   row k, and len becomes k.  Rows at or after the new len keep their bytes,
+ *   but hold nothing: the pages past the first ceil(k / page_size) are free
+ *   for other tables when the call's work is done.
+ * Only rows whose place lies beyond the budget move (order-preserving
+ * compaction moves every row after the first evicted one).
+ *
+ *  budget int32 [num_seqs][num_layers]; recent, sink >= 0.
+ *  ws  lethe_paged_evict_workspace_bytes(cache) bytes.
+ * A sequence with len out of range or a page out of range among its live rows
+ * sets LETHE_DEV_BAD_LAYOUT and is left alone in that layer.  The tokens of a
+ * segment's rows are distinct (appending makes them so).  Errors:
+ * LETHE_ERR_INVALID, LETHE_ERR_UNSUPPORTED, LETHE_ERR_WORKSPACE,
+ * LETHE_ERR_HIP.
+ */
+lethe_status lethe_paged_evict(const lethe_paged_cache* cache, const int32_t* budget, int32_t recent, int32_t sink,
+                               void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of lethe_paged_evict; 0 for an invalid description. */
+size_t lethe_paged_evict_workspace_bytes(const lethe_paged_cache* cache);
 
 /* Static, human-readable name of a status code. */
 const char* lethe_status_string(lethe_status status);

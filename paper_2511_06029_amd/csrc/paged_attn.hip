@@ -1,0 +1,1268 @@
+// Causal attention of a batch's newest rows over a paged cache, with the
+// importance update of Eq. 5 / Eq. 2, gfx950.
+//
+// The q_len queries of a sequence and the G query heads of a KV group are the
+// columns of one product: column c is query c / G, head c % G, so a group's
+// keys and values are read once for all of them whatever G and q_len are.
+//
+// One query a sequence (max_q_len <= 1), bound by the rows' bytes:
+//  1. decode_kernel: the rows of every (sequence, KV head) cut into chunks of
+//     like length, one block each; a wavefront takes 32 rows at a time on
+//     16x16x32 products, G columns of 16 in use.  Writes a chunk's (max, sum,
+//     output) and, for the scores, the rows' logits.
+//  2. finish_kernel: joins a segment's chunks and turns the logits into
+//     weights once the segment's max and sum are known.
+//
+// Longer queries, bound by the products:
+//  1. plan_kernel (one block): cuts every (sequence, 128 columns) into key
+//     ranges of like work and orders them, longest first.
+//  2. tile_kernel: flash attention forward of 128 columns over a key range,
+//     32 columns a wavefront on 32x32x16 products, keys and values shared by
+//     the block's four wavefronts through LDS.
+//  3. join_kernel: where a tile's keys were cut.
+//  4. seed_kernel (with scores): key-major second pass, the columns' final
+//     max and sum at hand, in a fixed order without atomics.
+#include <algorithm>
+
+#include "paged_internal.h"
+#include "paged_mma.h"
+
+namespace lethe {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kNumWaves = kThreads / kWave;
+constexpr float kNegBig = -1.0e30f;
+
+// Sizes of sequence b as this call sees them; ok: they fit together.
+struct AttnSeq {
+  int n, ql;
+  long long q0;
+  bool ok;
+};
+
+__device__ inline AttnSeq attn_seq(const PagedAttnArgs& a, int b) {
+  AttnSeq s;
+  s.n = a.c.len[b];
+  s.ql = a.q_len[b];
+  s.q0 = a.q_start[b];
+  s.ok = s.n >= 0 && s.n <= a.max_kv && s.ql >= 0 && s.ql <= s.n && s.ql <= a.max_q && s.q0 >= 0 &&
+         s.q0 + s.ql <= a.q_rows;
+  return s;
+}
+
+// Rows are addressed in granules of 16, which lie in one page whatever its
+// size: pool row of granule `g` (its rows 16 g ..), or -1 (flagged) where the
+// page is out of range.
+__device__ inline int granule_row(const PagedView& c, int b, int h, int g) {
+  const int row = 16 * g;
+  const int page = c.table[(long long)b * c.max_pages + (row >> c.page_shift)];
+  if (page < 0 || page >= c.num_pages) {
+    atomicOr(c.dev_status, LETHE_DEV_BAD_LAYOUT);
+    return -1;
+  }
+  return page_row(c, page, h) + (row & ((1 << c.page_shift) - 1));
+}
+
+// A raw product in base-2 logits: scaled, or scaled and capped,
+// cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)).
+template <bool kCap>
+__device__ inline float logit2(const PagedAttnArgs& a, float x) {
+  if constexpr (kCap)
+    return fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + hw_exp2(x * a.cap_in)), a.cap_log2);
+  else
+    return x * a.scale_log2;
+}
+
+__device__ inline float max_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// 16 bytes a lane from `base + off` into LDS: lane l's land at dst + 16 l.
+__device__ inline void load_lds(const char* p, lds_char* dst) {
+  __builtin_amdgcn_global_load_lds((global_cvoid*)p, (lds_void*)dst, 16, 0, 0);
+}
+
+__device__ inline void wait_vmem() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
+
+// ---------------------------------------------------------------------------
+// One query a sequence
+// ---------------------------------------------------------------------------
+constexpr int kDecStep = 32;        // rows a wavefront takes at a time
+constexpr int kDecMaxChunks = 64;   // of a segment
+constexpr int kDecChunkSteps = 14;  // steps of a chunk, where there are enough
+constexpr int kDecLeastSteps = 4;   // one a wavefront
+constexpr int kDecMinBlocks = 512, kDecMaxBlocks = 4096;
+constexpr int kFinRows = 1024;      // rows of a finishing block
+
+__host__ __device__ inline long long dec_blocks(long long steps) {
+  const long long nb = steps / kDecChunkSteps;
+  return nb < kDecMinBlocks ? kDecMinBlocks : nb > kDecMaxBlocks ? kDecMaxBlocks : nb;
+}
+// Floats of a chunk's partial: (max, sum) and output of every head.
+__host__ __device__ inline int dec_part(int G, int D) { return (G * (D + 2) + 31) / 32 * 32; }
+__host__ __device__ inline int dec_logits(int G) { return G <= 4 ? 4 : 8; }  // floats of a row
+
+struct DecChunk {
+  int b, h, c, nch, n;
+  int first;               // block index of the segment's chunk 0
+  long long row0;          // the segment's first row in the logits
+  long long q0;
+};
+
+// The chunk that block `idx` works on.  Every wave derives the same map: 64
+// sequences at a time, lane l holding sequence 64 r + l.  seg >= 0 asks for
+// chunk 0 of that segment (b HK + h) instead.
+template <int R>
+__device__ inline bool dec_chunk(const PagedAttnArgs& a, int idx, int seg, DecChunk& ck) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int steps[R], rows[R];
+  int total = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int b = kWave * r + lane;
+    steps[r] = rows[r] = 0;
+    if (b < a.c.B) {
+      const AttnSeq s = attn_seq(a, b);
+      if (s.ok && s.ql > 0) {
+        rows[r] = s.n;
+        steps[r] = (s.n + kDecStep - 1) / kDecStep;
+      } else if (!s.ok && blockIdx.x == 0 && threadIdx.x < kWave) {
+        atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
+      }
+    }
+    total += steps[r];
+  }
+  for (int o = kWave / 2; o > 0; o >>= 1) total += __shfl_xor(total, o);
+  const long long all = (long long)total * a.c.HK;
+  const int per = (int)max((long long)kDecLeastSteps, (all + dec_blocks(all) - 1) / dec_blocks(all));
+  int blocks0 = 0;
+  long long steps0 = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int nch = steps[r] == 0 ? 0 : min((steps[r] + per - 1) / per, kDecMaxChunks);
+    const int incl = wave_incl_scan_i32(nch * a.c.HK);
+    const int sincl = wave_incl_scan_i32(steps[r]);
+    const int sum = __builtin_amdgcn_readlane(incl, kWave - 1);
+    const bool mine = seg >= 0 ? seg / a.c.HK / kWave == r : idx < blocks0 + sum;
+    if (mine) {
+      const int l = seg >= 0 ? seg / a.c.HK % kWave : (int)__builtin_ctzll(__ballot(blocks0 + incl > idx));
+      ck.b = kWave * r + l;
+      ck.nch = __builtin_amdgcn_readlane(nch, l);
+      ck.n = __builtin_amdgcn_readlane(rows[r], l);
+      const int st = __builtin_amdgcn_readlane(steps[r], l);
+      if (ck.nch == 0) return false;
+      const int at = blocks0 + __builtin_amdgcn_readlane(incl, l) - ck.nch * a.c.HK;
+      ck.h = seg >= 0 ? seg % a.c.HK : (idx - at) / ck.nch;
+      ck.c = seg >= 0 ? 0 : (idx - at) % ck.nch;
+      ck.first = at + ck.h * ck.nch;
+      ck.row0 = ((steps0 + __builtin_amdgcn_readlane(sincl, l) - st) * a.c.HK + (long long)ck.h * st) * kDecStep;
+      ck.q0 = a.q_start[ck.b];
+      return true;
+    }
+    blocks0 += sum;
+    steps0 += __builtin_amdgcn_readlane(sincl, kWave - 1);
+  }
+  return false;
+}
+
+template <int D>
+struct DecCfg {
+  static constexpr int KK = D / 32;          // k-steps of 32 over the head dim
+  static constexpr int NT = D / 16;          // output tiles of 16 dims
+  static constexpr int ROWB = D * 2;
+  static constexpr int LPR = ROWB / 16;      // lanes a row for V loads
+  static constexpr int VLOADS = kDecStep * LPR / kWave;
+  // V load u carries rows u + VLOADS j into block u; the blocks' padding
+  // spreads the rows of one transposing read over the LDS banks.
+  static constexpr int VBLK = kWave * 16 + 32;
+  static constexpr int VTILE = VLOADS * VBLK;
+  static __device__ constexpr int vaddr(int r, int c) { return (r % VLOADS) * VBLK + (r / VLOADS) * ROWB + c; }
+};
+
+struct DecWs {
+  float* part;
+  float* logit;
+  long long logit_rows;
+};
+// Whether the workspace has room for the segment's logits: always, unless
+// tables share pages, which a call that updates scores does not allow.
+__device__ inline bool dec_room(const DecWs& ws, const DecChunk& ck) {
+  return ck.row0 + (ck.n + kDecStep - 1) / kDecStep * kDecStep <= ws.logit_rows;
+}
+
+template <typename T, int D, bool kCap, int R>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void decode_kernel(PagedAttnArgs a, DecWs ws) {
+  using Cfg = DecCfg<D>;
+  using M = Mma<T>;
+  constexpr int KK = Cfg::KK, NT = Cfg::NT, ROWB = Cfg::ROWB, LPR = Cfg::LPR, VLOADS = Cfg::VLOADS;
+  constexpr int kMaxG = 8;
+  __shared__ __attribute__((aligned(16))) char vtiles[kNumWaves * Cfg::VTILE];
+  __shared__ float2 wave_ml[kNumWaves][kMaxG];
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int g4 = lane >> 4, s = lane & 15;
+  DecChunk ck;
+  if (!dec_chunk<R>(a, blockIdx.x, -1, ck)) return;
+  const int G = a.G;
+  const int n = ck.n;
+  const int steps = (n + kDecStep - 1) / kDecStep;
+  const int first = (int)((long long)steps * ck.c / ck.nch), end = (int)((long long)steps * (ck.c + 1) / ck.nch);
+  lds_char* const vb = (lds_char*)vtiles + w * Cfg::VTILE;
+
+  // Queries as the B operand of S^T = K Q^T: lane (g4, s) holds
+  // Q[head s][dims 32 kk + 8 g4 ..], heads past G zero.
+  typename M::x8 qb[KK];
+  {
+    const char* q = (const char*)a.q + (ck.q0 * a.c.HQ + (long long)ck.h * G) * ROWB;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qb[kk] = s < G ? *reinterpret_cast<const typename M::x8*>(q + s * ROWB + 64 * kk + 16 * g4) : mma_zero<T>();
+  }
+
+  // Granules of this wave's next 32 steps, two a step: lane 2 i + g holds
+  // granule g of its i-th step from `base`.
+  int ids = -1;
+  bool bad = false;
+  auto load_ids = [&](int step) {
+    const int st = step + kNumWaves * (lane >> 1);
+    const int g = min(2 * st + (lane & 1), (n - 1) >> 4);
+    ids = granule_row(a.c, ck.b, ck.h, g);
+    bad = __any(ids < 0);
+  };
+  typename M::x8 kr[2][KK];
+  int g0 = 0, g1 = 0;
+  auto granules = [&](int i) {
+    g0 = __builtin_amdgcn_readlane(ids, 2 * i);
+    g1 = __builtin_amdgcn_readlane(ids, 2 * i + 1);
+  };
+  // Rows past the last one read that one instead; a granule out of range
+  // reads the pool's first rows.
+  auto row_of = [&](int base, int r) {
+    r = min(r, n - 1 - base);
+    return (long long)(max(r < 16 ? g0 : g1, 0) + (r & 15)) * ROWB;
+  };
+  auto load_k = [&](int base) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* p = a.c.k + row_of(base, 16 * t + s) + 16 * g4;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) kr[t][kk] = *reinterpret_cast<const typename M::x8*>(p + 64 * kk);
+    }
+  };
+  auto load_v = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < VLOADS; ++u)
+      load_lds(a.c.v + row_of(base, u + VLOADS * (lane / LPR)) + 16 * (lane % LPR), vb + u * Cfg::VBLK);
+  };
+
+  float m = kNegBig, l = 0.0f;
+  mma_f32x4_t o[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) o[nt] = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  const int lstride = dec_logits(G);
+  float* const logit = a.gamma > 0.0f && dec_room(ws, ck) ? ws.logit + ck.row0 * lstride : nullptr;
+
+  int step = first + w, i = 0;
+  if (step < end) {
+    load_ids(step);
+    granules(0);
+    load_k(step * kDecStep);
+    load_v(step * kDecStep);
+  }
+  while (step < end) {
+    const int base = step * kDecStep;
+    const int next = step + kNumWaves;
+    const bool b0 = bad && g0 < 0, b1 = bad && g1 < 0;  // of this step
+    // Rows of the step that take no part (wave-uniform).
+    const uint32_t dead = (n - base < kDecStep ? ~0u << (n - base) : 0u) | (b0 ? 0xffffu : 0u) | (b1 ? 0xffff0000u : 0u);
+    mma_f32x4_t x[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      x[t] = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) x[t] = M::mma16(kr[t][kk], qb[kk], x[t]);
+    }
+    if (logit) {
+      // The other orientation: lane (g4 < 2, s) gets heads 4 g4 .. + 3 of row
+      // 16 t + s, one 16-byte store.
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        mma_f32x4_t y = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) y = M::mma16(qb[kk], kr[t][kk], y);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = logit2<kCap>(a, y[r]);
+        const int row = base + 16 * t + s;
+        if (4 * g4 < lstride && row < n) *reinterpret_cast<mma_f32x4_t*>(logit + (long long)row * lstride + 4 * g4) = y;
+      }
+    }
+    if (next < end) {
+      if (++i == kWave / 2) {
+        load_ids(next);
+        i = 0;
+      }
+      granules(i);
+      load_k(next * kDecStep);
+    }
+    // Logits of rows base + 16 t + 4 g4 + r for head s.
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = logit2<kCap>(a, x[t][r]);
+        if (dead && ((dead >> (16 * t + 4 * g4 + r)) & 1u)) x[t][r] = -INFINITY;
+      }
+    float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
+                     fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float mnew = fmaxf(m, mx);
+    const float corr = hw_exp2(m - mnew);
+    m = mnew;
+    float psum = 0.0f;
+    typename M::x8 p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float e = hw_exp2(x[j >> 2][j & 3] - mnew);
+      psum += e;
+      p[j] = (T)e;
+    }
+    l = l * corr + psum;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) o[nt] *= corr;
+    // V^T operand through the transposing LDS read: lane s of group g4 points
+    // at row 4 g4 + s / 4 (and 16 more), column 16 nt + 4 (s % 4); its slots
+    // j < 4 are rows 4 g4 + j, the others 16 + 4 g4 + j - 4, as p's.
+    const int rsub = 4 * g4 + (s >> 2);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int col = (16 * nt + 4 * (s & 3)) * 2;
+      const typename M::x4 a0 = M::read_tr(vb + Cfg::vaddr(rsub, col)), a1 = M::read_tr(vb + Cfg::vaddr(rsub + 16, col));
+      typename M::x8 av = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+      if (dead) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if ((dead >> (16 * (j >> 2) + 4 * g4 + (j & 3))) & 1u) av[j] = (T)0.0f;
+      }
+      o[nt] = M::mma16(av, p, o[nt]);
+    }
+    if (next < end) {
+      // The tile's reads are done (their results are in the products above).
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+      load_v(next * kDecStep);
+    }
+    step = next;
+  }
+
+  // Lane groups hold different rows of the same heads.
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  // The waves' parts of the chunk, joined in LDS: outputs transposed through
+  // this wave's own V tile, [head][dim].
+  if (g4 == 0 && s < G) wave_ml[w][s] = make_float2(m, l);
+  static_assert(Cfg::VTILE >= kMaxG * D * 4, "a wave's outputs fit its V tile");
+  wait_vmem();
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  if (s < G) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      *(__attribute__((address_space(3))) mma_f32x4_t*)(vb + (s * D + 16 * nt + 4 * g4) * 4) = o[nt];
+  }
+  __syncthreads();
+  float* const part = ws.part + (long long)blockIdx.x * dec_part(G, D);
+  for (int x = tid; x < G * D; x += kThreads) {
+    const int g = x / D;
+    float mm = wave_ml[0][g].x;
+#pragma unroll
+    for (int v = 1; v < kNumWaves; ++v) mm = fmaxf(mm, wave_ml[v][g].x);
+    float sum = 0.0f, lsum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < kNumWaves; ++v) {
+      const float f = hw_exp2(wave_ml[v][g].x - mm);
+      sum = fmaf(f, *reinterpret_cast<const float*>(vtiles + v * Cfg::VTILE + x * 4), sum);
+      lsum = fmaf(f, wave_ml[v][g].y, lsum);
+    }
+    part[2 * G + x] = sum;
+    if (x % D == 0) *reinterpret_cast<float2*>(part + 2 * g) = make_float2(mm, lsum);
+  }
+}
+
+// blockIdx.x = segment, blockIdx.y = range of kFinRows rows.  Every block
+// joins the chunks' statistics; the first one of a segment the outputs too.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs ws) {
+  constexpr int kMaxG = 8;
+  __shared__ float factor[kDecMaxChunks][kMaxG];  // what a chunk's output counts
+  __shared__ float2 stat[kMaxG];                  // max, 1 / sum
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
+  DecChunk ck;
+  if (!dec_chunk<R>(a, -1, blockIdx.x, ck)) return;
+  const long long r0 = (long long)blockIdx.y * kFinRows;
+  if (r0 >= ck.n) return;
+  const int G = a.G, pstride = dec_part(G, D);
+  const float* const part = ws.part + (long long)ck.first * pstride;
+  for (int g = w; g < G; g += kNumWaves) {
+    const float2 ml = lane < ck.nch ? *reinterpret_cast<const float2*>(part + (long long)lane * pstride + 2 * g)
+                                    : make_float2(kNegBig, 0.0f);
+    const float mm = wave_max(ml.x);
+    const float f = hw_exp2(ml.x - mm);
+    const float sum = wave_sum(f * ml.y);
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // no row at all: 0
+    factor[lane][g] = f * inv;
+    if (lane == 0) stat[g] = make_float2(mm, inv);
+  }
+  __syncthreads();
+  if (r0 == 0) {
+    T* const out = (T*)a.out + (ck.q0 * a.c.HQ + (long long)ck.h * G) * D;
+    for (int x = tid; x < G * D; x += kThreads) {
+      const int g = x / D;
+      float sum = 0.0f;
+#pragma unroll 4
+      for (int c = 0; c < ck.nch; ++c) sum = fmaf(factor[c][g], part[(long long)c * pstride + 2 * G + x], sum);
+      out[x] = (T)sum;
+    }
+  }
+  if (!(a.gamma > 0.0f)) return;
+  if (!dec_room(ws, ck)) {
+    if (tid == 0) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
+    return;
+  }
+  const int ls = dec_logits(G);
+  const float* const logit = ws.logit + ck.row0 * ls;
+  const int mask = (1 << a.c.page_shift) - 1;
+#pragma unroll
+  for (int i = 0; i < kFinRows / kThreads; ++i) {
+    const int r = (int)r0 + i * kThreads + tid;
+    if (r < ck.n) {
+      const int page = a.c.table[(long long)ck.b * a.c.max_pages + (r >> a.c.page_shift)];
+      if (page >= 0 && page < a.c.num_pages) {
+        float* const sp = a.c.score + page_row(a.c, page, ck.h) + (r & mask);
+        float acc = 0.0f;
+        for (int g0 = 0; g0 < G; g0 += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(logit + (long long)r * ls + g0);
+          const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            if (g0 + g < G) acc = fmaf(hw_exp2(xs[g] - stat[g0 + g].x), stat[g0 + g].y, acc);
+        }
+        *sp = fmaf(a.gamma, *sp, acc);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Longer queries
+// ---------------------------------------------------------------------------
+constexpr int kTileCols = 128;    // columns of a block
+constexpr int kKeyStep = 64;      // keys of a step
+constexpr int kLeastKeys = 512;   // of a key range
+constexpr int kRanges = 1024;     // blocks that the ranges aim at
+constexpr int kMaxSplit = 64;     // ranges of a tile
+constexpr int kPlanThreads = 1024;
+constexpr int kBuckets = 1024;
+
+struct PlanHead {
+  int items, splits;  // entries of the two lists
+};
+// One tile and key range, or (splits) one tile with several ranges.
+struct PlanItem {
+  int b, tile;
+  int range;   // or, in the split list, how many
+  int slot;    // of its partial, -1: the only range
+};
+
+struct TileWs {
+  PlanHead* head;
+  int32_t* keys;     // [B] keys of a range
+  PlanItem* items;
+  PlanItem* splits;
+  float2* stat;      // [q_rows][HQ] max (base 2), 1 / sum
+  float2* part_ml;   // [slots][HK][128]
+  float* part_o;     // [slots][HK][128][D]
+  int max_items, max_slots;
+};
+
+__device__ inline int tile_count(int cols) { return (cols + kTileCols - 1) / kTileCols; }
+// One past the last key that columns up to `last` attend.
+__device__ inline int key_end(const AttnSeq& s, int last, int G) { return s.n - s.ql + min(last / G, s.ql - 1) + 1; }
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, TileWs ws) {
+  __shared__ long long scan_tmp[kPlanThreads / kWave + 1];
+  __shared__ int item0[kPlanThreads];       // first item of a sequence
+  __shared__ int split0[kPlanThreads];      // its first entry in the split list
+  __shared__ int slot0[kPlanThreads];       // its first partial
+  __shared__ int keys_of[kPlanThreads];     // keys of a range
+  __shared__ int hist[kBuckets];
+  const int tid = threadIdx.x;
+  AttnSeq s{0, 0, 0, true};
+  if (tid < a.c.B) s = attn_seq(a, tid);
+  if (!s.ok) {
+    atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
+    s.n = s.ql = 0;
+  }
+  const int tiles = tile_count(s.ql * a.G);
+  long long work;
+  block_excl_scan<kPlanThreads>((long long)tiles * a.c.HK * s.n, scan_tmp, &work);
+  const long long want = max((long long)kLeastKeys, (work + kRanges - 1) / kRanges);
+  const int ranges = tiles ? (int)min((long long)kMaxSplit, (s.n + want - 1) / want) : 1;
+  const int keys = (int)((((long long)s.n + ranges - 1) / ranges + kKeyStep - 1) / kKeyStep * kKeyStep);
+  if (tid < a.c.B) ws.keys[tid] = keys;
+  keys_of[tid] = keys;
+  long long total, splits, slots;
+  item0[tid] = (int)block_excl_scan<kPlanThreads>((long long)tiles * ranges, scan_tmp, &total);
+  split0[tid] = (int)block_excl_scan<kPlanThreads>(ranges > 1 ? tiles : 0, scan_tmp, &splits);
+  slot0[tid] = (int)block_excl_scan<kPlanThreads>(ranges > 1 ? (long long)tiles * ranges : 0, scan_tmp, &slots);
+  // More work than the bounds allow: rows of q that belong to two sequences.
+  const bool over = total > ws.max_items || slots > ws.max_slots;
+  const int items = over ? 0 : (int)total;
+  hist[tid] = 0;
+  if (tid == 0) {
+    if (over) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
+    ws.head->items = items;
+    ws.head->splits = over ? 0 : (int)splits;
+  }
+  __syncthreads();
+  // Item i: its sequence by bisection, then tile and range; keys it works on.
+  auto item = [&](int i, PlanItem& it) {
+    int lo = 0, hi = a.c.B;  // item0[lo] <= i < item0[hi] (empty sequences share a start)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (item0[mid] <= i)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const AttnSeq q = attn_seq(a, lo);
+    const int per = keys_of[lo];
+    const int nr = (int)(((lo + 1 < kPlanThreads ? item0[lo + 1] : items) - item0[lo]) / tile_count(q.ql * a.G));
+    it.b = lo;
+    it.tile = (i - item0[lo]) / nr;
+    it.range = (i - item0[lo]) % nr;
+    it.slot = nr > 1 ? slot0[lo] + i - item0[lo] : -1;
+    const int end = key_end(q, kTileCols * it.tile + kTileCols - 1, a.G);
+    const long long from = (long long)it.range * per;
+    if (it.range == 0 && nr > 1) {
+      const PlanItem sp{lo, it.tile, (int)((end + per - 1) / per), slot0[lo] + it.tile * nr};
+      ws.splits[split0[lo] + it.tile] = sp;
+    }
+    return from >= end ? 0 : (int)(min((long long)end, from + per) - from);
+  };
+  auto bucket = [&](int keyn) { return kBuckets - 1 - min(keyn / kKeyStep, kBuckets - 1); };
+  for (int i = tid; i < items; i += kPlanThreads) {
+    PlanItem it;
+    atomicAdd(&hist[bucket(item(i, it))], 1);
+  }
+  __syncthreads();
+  long long unused;
+  const int before = (int)block_excl_scan<kPlanThreads>(hist[tid], scan_tmp, &unused);
+  hist[tid] = before;
+  __syncthreads();
+  for (int i = tid; i < items; i += kPlanThreads) {
+    PlanItem it;
+    const int keyn = item(i, it);
+    const int at = atomicAdd(&hist[bucket(keyn)], 1);  // the order within a bucket does not matter
+    if (keyn == 0) it.tile = -1;
+    ws.items[at] = it;
+  }
+}
+
+template <int D>
+struct TileCfg {
+  static constexpr int KS = D / 16;          // k-steps of 16 over the head dim
+  static constexpr int NT = D / 32;          // output tiles of 32 dims
+  static constexpr int ROWB = D * 2;
+  static constexpr int CH = ROWB / 16;       // 16-byte pieces of a row
+  // K tiles: piece c of row r at 16-byte slot r CH + (c ^ (r mod CH)), so the
+  // rows that an operand read touches fall in different LDS banks.
+  static constexpr int KTILE = kKeyStep * ROWB;
+  static constexpr int KPW = KTILE / (kThreads * 16);  // loads of a wave
+  static __device__ constexpr int kslot(int r, int c) { return r * CH + (c ^ (r % CH)); }
+  // V tiles: load u (one wavefront) carries rows u + VLOADS j into block u.
+  static constexpr int VLOADS = kKeyStep * CH / kWave;
+  static constexpr int VPW = VLOADS / kNumWaves;
+  static constexpr int VBLK = kWave * 16 + 64;
+  static constexpr int VTILE = VLOADS * VBLK;
+  static __device__ constexpr int vaddr(int r, int c) { return (r % VLOADS) * VBLK + (r / VLOADS) * ROWB + c; }
+};
+
+template <typename T, int D, bool kCap>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(PagedAttnArgs a, TileWs ws) {
+  using Cfg = TileCfg<D>;
+  using M = Mma<T>;
+  constexpr int KS = Cfg::KS, NT = Cfg::NT, ROWB = Cfg::ROWB, CH = Cfg::CH, STEP = kKeyStep;
+  constexpr int KPW = Cfg::KPW, VPW = Cfg::VPW;
+  __shared__ __attribute__((aligned(16))) char ktile0[Cfg::KTILE];
+  __shared__ __attribute__((aligned(16))) char ktile1[Cfg::KTILE];
+  __shared__ __attribute__((aligned(16))) char vtile0[Cfg::VTILE];
+  __shared__ __attribute__((aligned(16))) char vtile1[Cfg::VTILE];
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int hh = lane >> 5;  // lane half
+  const int s = lane & 31;   // column
+  const int h = blockIdx.x % a.c.HK;
+  const int at = blockIdx.x / a.c.HK;
+  if (at >= ws.head->items) return;
+  const PlanItem it = ws.items[at];
+  if (it.tile < 0) return;
+  const int b = it.b, G = a.G, HQ = a.c.HQ;
+  const AttnSeq sq = attn_seq(a, b);
+  const int cols = sq.ql * G, first = sq.n - sq.ql;
+  const int ks = it.range * ws.keys[b];
+  // Keys [ks, kend) of this wave and of the block; rows up to `full` are
+  // attended by each of the wave's columns.
+  const int range_end = (int)min((long long)ks + ws.keys[b], (long long)sq.n);
+  const int c0 = kTileCols * it.tile + 32 * w;
+  const bool active = c0 < cols;
+  const int kend_blk = min(range_end, key_end(sq, kTileCols * it.tile + kTileCols - 1, G));
+  const int kend = active ? min(range_end, key_end(sq, c0 + 31, G)) : 0;
+  const int full = first + c0 / G;
+  const int nsteps = (kend_blk - ks + STEP - 1) / STEP;
+  const int own = kend > ks ? (kend - ks + STEP - 1) / STEP : 0;
+  const int col = c0 + s;
+  const int pos = first + col / G;  // this lane's last key
+  const float sc = kCap ? 1.0f : a.scale_log2;
+
+  // Queries as the B operand of S^T = K Q^T: lane (hh, s) holds
+  // Q[column s][dims 16 kk + 8 hh ..].
+  typename M::x8 qb[KS];
+  {
+    const char* q = (const char*)a.q + ((sq.q0 + col / G) * HQ + h * G + col % G) * (long long)ROWB;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk)
+      qb[kk] = col < cols ? *reinterpret_cast<const typename M::x8*>(q + 32 * kk + 16 * hh) : mma_zero<T>();
+  }
+
+  // Granules of 16 steps at a time: lane l holds granule l of the window; even
+  // windows in ids[0], odd ones in ids[1], the next one asked for a window
+  // ahead.
+  const int glast = (kend_blk - 1) >> 4;
+  int ids0 = -1, ids1 = -1;
+  bool bad = false;
+  auto load_ids = [&](int window, int& ids) {
+    ids = granule_row(a.c, b, h, min((ks >> 4) + kWave * window + lane, glast));
+    bad = bad || __any(ids < 0);
+  };
+  auto granule = [&](int st, int g) {
+    return __builtin_amdgcn_readlane((st >> 4) & 1 ? ids1 : ids0, 4 * (st & 15) + g);
+  };
+  // This wave's share of a step's tiles.  Rows past the last key of the block
+  // (final step only) read that key instead; a granule out of range the
+  // pool's first rows.
+  const int krow = (kWave * w + lane) / CH;
+  const int kpiece = 16 * ((lane % CH) ^ (krow % CH));
+  auto issue_k = [&](int st, char* tile) {
+    const int j0 = ks + st * STEP;
+    if (j0 >= kend_blk) return;
+    lds_char* kl = (lds_char*)tile + kWave * 16 * w;
+    const int last = kend_blk - 1 - j0;
+#pragma unroll
+    for (int k = 0; k < KPW; ++k) {
+      constexpr int RPL = kThreads / CH;              // rows between a wave's loads
+      const int g = (RPL * k + kWave / CH * w) >> 4;  // uniform: a load stays in a granule
+      if (last >= STEP - 1) {
+        const char* p = a.c.k + (long long)max(granule(st, g), 0) * ROWB;
+        load_lds(p + (unsigned)((krow & 15) * ROWB + kpiece), kl + kWave * 16 * kNumWaves * k);
+      } else {
+        const int r = min(krow + RPL * k, last);
+        const char* p = a.c.k + (long long)max(granule(st, min(g, last >> 4)), 0) * ROWB;
+        load_lds(p + (unsigned)((r & 15) * ROWB + kpiece), kl + kWave * 16 * kNumWaves * k);
+      }
+    }
+  };
+  const int vrow = w + Cfg::VLOADS * (lane / CH);  // + 4 a load; granule lane / 16
+  auto issue_v = [&](int st, char* tile) {
+    const int j0 = ks + st * STEP;
+    if (j0 >= kend_blk) return;
+    lds_char* vl = (lds_char*)tile + Cfg::VBLK * w;
+    const int last = kend_blk - 1 - j0;
+    const int i0 = granule(st, 0), i1 = granule(st, 1), i2 = granule(st, 2), i3 = granule(st, 3);
+    if (last >= STEP - 1) {
+      const int g = lane >> 4;
+      const int row = max(g < 2 ? (g == 0 ? i0 : i1) : (g == 2 ? i2 : i3), 0);
+      const char* p = a.c.v + (long long)row * ROWB + (vrow & 15) * ROWB + 16 * (lane % CH);
+#pragma unroll
+      for (int k = 0; k < VPW; ++k) load_lds(p + k * kNumWaves * ROWB, vl + Cfg::VBLK * kNumWaves * k);
+    } else {
+#pragma unroll
+      for (int k = 0; k < VPW; ++k) {
+        const int r = min(vrow + kNumWaves * k, last);
+        const int g = r >> 4;
+        const int row = max(g < 2 ? (g == 0 ? i0 : i1) : (g == 2 ? i2 : i3), 0) + (r & 15);
+        load_lds(a.c.v + (long long)row * ROWB + 16 * (lane % CH), vl + Cfg::VBLK * kNumWaves * k);
+      }
+    }
+  };
+
+  float m = kNegBig, l = 0.0f, corr = 1.0f;
+  mma_f32x16_t o[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[nt][r] = 0.0f;
+  // S^T of a step: lane (hh, s), register r of sub-tile t: key j0 + 32 t +
+  // 8 (r / 4) + 4 hh + r % 4, column s.
+  mma_f32x16_t sa[2], sb[2];
+  auto clear = [&](mma_f32x16_t (&x)[2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[t][r] = 0.0f;
+  };
+  auto qk = [&](mma_f32x16_t (&x)[2], const char* kt, int kk) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      x[t] = M::mma32(*reinterpret_cast<const typename M::x8*>(kt + 16 * Cfg::kslot(32 * t + s, 2 * kk + hh)), qb[kk], x[t]);
+  };
+  // Rows of step st on pages out of range, as bits of its granules.
+  auto bad_granules = [&](int st) {
+    unsigned x = 0;
+    if (bad) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) x |= (granule(st, g) < 0 ? 1u : 0u) << g;
+    }
+    return x;
+  };
+  // A step is plain where every one of its rows counts for every column.
+  auto plain = [&](int st) { return ks + st * STEP + STEP - 1 <= full && ks + (st + 1) * STEP <= kend && !bad; };
+  auto logits = [&](mma_f32x16_t (&x)[2], int st) {
+    if constexpr (kCap) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[t][r] = logit2<true>(a, x[t][r]);
+    }
+    if (!plain(st)) {
+      const int j0 = ks + st * STEP;
+      const int lim = min(pos, kend - 1) - j0 - 4 * hh;
+      const unsigned bg = bad_granules(st);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * t + 8 * (r >> 2) + (r & 3) > lim || ((bg >> (2 * t + (r >> 3))) & 1u)) x[t][r] = -INFINITY;
+    }
+    float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, x[0][r]), x[1][r]);
+    const float mnew = fmaxf(m, max_halves(mx) * sc);
+    corr = hw_exp2(m - mnew);
+    m = mnew;
+  };
+  // Once the running maxima settle most steps leave every lane's correction at
+  // exactly 1; the wave then skips the rescale.
+  auto rescale = [&]() {
+    if (__any(corr != 1.0f)) {
+      l *= corr;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[nt][r] *= corr;
+    }
+  };
+  // Weights of keys 16 mm .. + 15 in the order of the V^T operand: slot j is
+  // key 4 hh + j (j < 4) or 8 + 4 hh + j - 4.  They are rounded to the
+  // storage type, as the output is; the sum is of the unrounded ones.
+  float psum[2];
+  auto weights = [&](const mma_f32x16_t (&x)[2], int mm) {
+    typename M::x8 p;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      const float pa = hw_exp2(fmaf(x[mm >> 1][8 * (mm & 1) + j], sc, -m));
+      const float pb = hw_exp2(fmaf(x[mm >> 1][8 * (mm & 1) + j + 1], sc, -m));
+      psum[0] += pa;
+      psum[1] += pb;
+      const typename M::x2 r = __builtin_convertvector((mma_f32x2_t{pa, pb}), typename M::x2);
+      p[j] = r[0];
+      p[j + 1] = r[1];
+    }
+    return p;
+  };
+  // V^T operand of keys 16 mm .. and dims 32 nt ..: lane i of a 16-lane group
+  // points at row 4 hh + i / 4 (and 8 more), 4 columns from
+  // 32 nt + 16 (group mod 2) + 4 (i mod 4).
+  auto v_operand = [&](const char* vtile, int mm, int nt) {
+    const lds_char* vt = (const lds_char*)vtile;
+    const int vr = 16 * mm + 4 * hh + ((lane & 15) >> 2);
+    const int c = (32 * nt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+    const typename M::x4 a0 = M::read_tr(vt + Cfg::vaddr(vr, c)), a1 = M::read_tr(vt + Cfg::vaddr(vr + 8, c));
+    return __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto pv = [&](const char* vtile, int mm, const typename M::x8& p) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) o[nt] = M::mma32(v_operand(vtile, mm, nt), p, o[nt]);
+  };
+  // A plain step that is not this wave's last: weights and P V of step st,
+  // whose logits are in sx, interleaved with S^T of step st + 1 (K runs one
+  // tile ahead of V).
+  auto body = [&](int st, mma_f32x16_t (&sx)[2], mma_f32x16_t (&sn)[2], const char* knext, const char* vcur) {
+    rescale();
+    clear(sn);
+    psum[0] = psum[1] = 0.0f;
+    typename M::x8 p = weights(sx, 0);
+#pragma unroll
+    for (int kk = 0; kk < KS / 4; ++kk) qk(sn, knext, kk);
+#pragma unroll
+    for (int mm = 1; mm < 4; ++mm) {
+      const typename M::x8 pn = weights(sx, mm);
+#pragma unroll
+      for (int kk = mm * KS / 4; kk < (mm + 1) * KS / 4; ++kk) qk(sn, knext, kk);
+      pv(vcur, mm - 1, p);
+      p = pn;
+    }
+    l += psum[0] + psum[1];
+    pv(vcur, 3, p);
+    logits(sn, st + 1);
+  };
+  // Rows of a step that some columns do not attend must not meet them in a
+  // product where they hold an infinity or NaN (0 times either is NaN).  Bits
+  // of the rows to leave out: those that no column of the wave attends, and
+  // of those that only some do the ones that hold such a value, which
+  // `apart` gets.
+  auto left_out = [&](int st, const char* vcur, unsigned long long& apart) {
+    const int j0 = ks + st * STEP;
+    const unsigned bg = bad_granules(st);
+    unsigned long long z = kend - j0 < STEP ? ~0ull << (kend - j0) : 0ull;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      if ((bg >> g) & 1u) z |= 0xffffull << (16 * g);
+    apart = 0;
+    const int r0 = max(full + 1 - j0, 0), r1 = min(kend - j0, STEP);  // attended by some columns only
+    for (int x0 = r0 * CH; x0 < r1 * CH; x0 += kWave) {
+      const int x = min(x0 + lane, r1 * CH - 1);
+      const uint4 v = *reinterpret_cast<const uint4*>(vcur + Cfg::vaddr(x / CH, 16 * (x % CH)));
+      const uint32_t e = M::kExpMask;
+      auto odd = [&](uint32_t u) { return (u & e) == e || ((u >> 16) & e) == e; };
+      unsigned long long hit = __ballot(odd(v.x) || odd(v.y) || odd(v.z) || odd(v.w));
+      while (hit) {  // rare
+        const int i = (int)__builtin_ctzll(hit);
+        apart |= 1ull << (min(x0 + i, r1 * CH - 1) / CH);
+        hit &= hit - 1;
+      }
+    }
+    apart &= ~z;
+    return z | apart;
+  };
+  // Any other step: S^T of the next one is not interleaved.
+  auto careful = [&](int st, const char* vcur) {
+    rescale();
+    psum[0] = psum[1] = 0.0f;
+    unsigned long long apart;
+    const unsigned long long z = left_out(st, vcur, apart);
+    typename M::x8 p[4];
+#pragma unroll
+    for (int mm = 0; mm < 4; ++mm) {
+      p[mm] = weights(sa, mm);
+      const unsigned zl = (unsigned)(z >> (16 * mm + 4 * hh));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        typename M::x8 av = v_operand(vcur, mm, nt);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if ((zl >> (8 * (j >> 2) + (j & 3))) & 1u) av[j] = (T)0.0f;
+        o[nt] = M::mma32(av, p[mm], o[nt]);
+      }
+    }
+    l += psum[0] + psum[1];
+    if (apart) {
+      // Their contributions one by one, to the columns that attend them.
+      float pw[32];
+#pragma unroll
+      for (int x = 0; x < 32; ++x) pw[x] = (float)p[x >> 3][x & 7];
+#pragma unroll 1
+      while (apart) {
+        const int r = (int)__builtin_ctzll(apart);
+        apart &= apart - 1;
+        const float mine = pw[8 * (r >> 4) + 4 * ((r >> 3) & 1) + (r & 3)];
+        const float other = __shfl_xor(mine, 32);
+        const float pr = ((r >> 2) & 1) == hh ? mine : other;
+        if (pos >= ks + st * STEP + r) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const int d = 32 * nt + 8 * (x >> 2) + 4 * hh + (x & 3);
+              o[nt][x] = fmaf(pr, (float)*reinterpret_cast<const T*>(vcur + Cfg::vaddr(r, 2 * d)), o[nt][x]);
+            }
+        }
+      }
+    }
+  };
+
+  // At step st, K of step st + 2 and V of step st + 1 are on their way into
+  // the buffers that step st - 1 has used.  Each wave waits for its own loads;
+  // the barrier makes every wave's visible and says that the buffers to fill
+  // have been read.
+  auto advance = [&](int st, char* kfill, char* vfill) {
+    wait_vmem();
+    __syncthreads();
+    if ((st & 15) == 0 && st > 0) {
+      if ((st >> 4) & 1)
+        load_ids((st >> 4) + 1, ids0);
+      else
+        load_ids((st >> 4) + 1, ids1);
+    }
+    issue_k(st + 2, kfill);
+    issue_v(st + 1, vfill);
+  };
+  load_ids(0, ids0);
+  load_ids(1, ids1);
+  issue_k(0, ktile0);
+  issue_k(1, ktile1);
+  issue_v(0, vtile0);
+  wait_vmem();
+  __syncthreads();
+  clear(sa);
+  if (own > 0) {
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) qk(sa, ktile0, kk);
+    logits(sa, 0);
+  }
+  // Steps before `lead` are plain and not the last.
+  int lead = min(own - 1, (min(full, kend - 1) + 1 - ks) / STEP);
+  if (bad) lead = 0;
+  int st = 0;
+  for (; st + 2 <= lead; st += 2) {
+    advance(st, ktile0, vtile1);
+    body(st, sa, sb, ktile1, vtile0);
+    advance(st + 1, ktile1, vtile0);
+    body(st + 1, sb, sa, ktile0, vtile1);
+    if (bad) break;  // a window further on has a page out of range
+  }
+  if (bad && st + 2 <= lead) {
+    st += 2;
+  } else if (st < lead) {
+    advance(st, ktile0, vtile1);
+    body(st, sa, sb, ktile1, vtile0);
+    ++st;
+    sa[0] = sb[0];
+    sa[1] = sb[1];
+  }
+  for (; st < own; ++st) {
+    advance(st, (st & 1) ? ktile1 : ktile0, (st & 1) ? vtile0 : vtile1);
+    careful(st, (st & 1) ? vtile1 : vtile0);
+    if (st + 1 < own) {
+      clear(sa);
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) qk(sa, (st & 1) ? ktile0 : ktile1, kk);
+      logits(sa, st + 1);
+    }
+  }
+  for (; st < nsteps; ++st) advance(st, (st & 1) ? ktile1 : ktile0, (st & 1) ? vtile0 : vtile1);
+  if (!active) return;
+
+  // l is split over the two lane halves of a column; m is common.
+  l += __shfl_xor(l, 32);
+  if (it.slot >= 0) {
+    const long long pc = ((long long)it.slot * a.c.HK + h) * kTileCols + 32 * w + s;
+    if (hh == 0) ws.part_ml[pc] = make_float2(m, l);
+    float* const po = ws.part_o + pc * D;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(po + 32 * nt + 2 * r + 4 * hh) = make_float4(o[nt][r], o[nt][r + 1], o[nt][r + 2], o[nt][r + 3]);
+    return;
+  }
+  if (col >= cols) return;
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no row at all: 0
+  const long long orow = (sq.q0 + col / G) * HQ + h * G + col % G;
+  T* const out = (T*)a.out + orow * D;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const mma_f32x4_t f = mma_f32x4_t{o[nt][r], o[nt][r + 1], o[nt][r + 2], o[nt][r + 3]} * inv;
+      *reinterpret_cast<typename M::x4*>(out + 32 * nt + 2 * r + 4 * hh) = __builtin_convertvector(f, typename M::x4);
+    }
+  if (hh == 0 && a.gamma > 0.0f) ws.stat[orow] = make_float2(m, inv);
+}
+
+// Tiles whose keys were cut: blockIdx.x = entry of the split list, .y = KV
+// head; four columns a wave at a time, 16 lanes each.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs ws) {
+  if ((int)blockIdx.x >= ws.head->splits) return;
+  const PlanItem it = ws.splits[blockIdx.x];
+  const int h = blockIdx.y, G = a.G;
+  const AttnSeq sq = attn_seq(a, it.b);
+  constexpr int EL = D / 16;  // dims of a lane
+  const int sub = threadIdx.x / 16, x = threadIdx.x % 16;
+  for (int c = sub; c < kTileCols; c += kThreads / 16) {
+    const int col = kTileCols * it.tile + c;
+    if (col >= sq.ql * G) break;
+    const long long p0 = ((long long)it.slot * a.c.HK + h) * kTileCols + c;
+    const long long ps = (long long)a.c.HK * kTileCols;
+    float m = kNegBig;
+    for (int r = 0; r < it.range; ++r) m = fmaxf(m, ws.part_ml[p0 + r * ps].x);
+    float l = 0.0f, o[EL];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) o[e] = 0.0f;
+    for (int r = 0; r < it.range; ++r) {
+      const float2 ml = ws.part_ml[p0 + r * ps];
+      const float f = hw_exp2(ml.x - m);
+      l = fmaf(f, ml.y, l);
+      const float4* const po = reinterpret_cast<const float4*>(ws.part_o + (p0 + r * ps) * D);
+#pragma unroll
+      for (int e = 0; e < EL; e += 4) {
+        const float4 v = po[x + 4 * e];
+        o[e] = fmaf(f, v.x, o[e]);
+        o[e + 1] = fmaf(f, v.y, o[e + 1]);
+        o[e + 2] = fmaf(f, v.z, o[e + 2]);
+        o[e + 3] = fmaf(f, v.w, o[e + 3]);
+      }
+    }
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    const long long orow = (sq.q0 + col / G) * a.c.HQ + h * G + col % G;
+    typedef typename Mma<T>::x4 x4;
+#pragma unroll
+    for (int e = 0; e < EL; e += 4) {
+      const mma_f32x4_t f = mma_f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]} * inv;
+      reinterpret_cast<x4*>((T*)a.out + orow * D)[x + 4 * e] = __builtin_convertvector(f, x4);
+    }
+    if (x == 0 && a.gamma > 0.0f) ws.stat[orow] = make_float2(m, inv);
+  }
+}
+
+// Second pass, key-major.  A block is four waves of 32 keys each times two
+// groups of waves; group ig takes the column tiles ig, ig + 2, ... of 32
+// columns and keeps its own double-buffered query tile.
+constexpr int kSeedWaves = 4, kSeedGroups = 2;
+constexpr int kSeedKeys = 32 * kSeedWaves;
+
+template <typename T, int D, bool kCap>
+__global__ __launch_bounds__(kWave* kSeedWaves* kSeedGroups) __attribute__((amdgpu_waves_per_eu(2))) void seed_kernel(
+    PagedAttnArgs a, TileWs ws) {
+  using Cfg = TileCfg<D>;
+  using M = Mma<T>;
+  constexpr int KS = Cfg::KS, ROWB = Cfg::ROWB, CH = Cfg::CH;
+  constexpr int QTILE = 32 * ROWB;
+  constexpr int LPW = QTILE / (kWave * 16) / kSeedWaves;  // loads of a wave
+  static_assert(LPW >= 1, "a tile gives every wave of a group a load");
+  __shared__ __attribute__((aligned(16))) char buf0[kSeedGroups * QTILE];
+  __shared__ __attribute__((aligned(16))) char buf1[kSeedGroups * QTILE];
+  __shared__ float sums[kSeedGroups][kSeedKeys];
+  const int tid = threadIdx.x;
+  const int lane = tid & (kWave - 1);
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int kw = w % kSeedWaves, ig = w / kSeedWaves;
+  const int hh = lane >> 5, s = lane & 31;
+  const int b = blockIdx.x / a.c.HK, h = blockIdx.x % a.c.HK;
+  const long long kb = ((long long)blockIdx.y + (long long)gridDim.y * blockIdx.z) * kSeedKeys;
+  const AttnSeq sq = attn_seq(a, b);
+  if (!sq.ok || sq.ql == 0 || kb >= sq.n) return;
+  const int G = a.G, HQ = a.c.HQ, cols = sq.ql * G, first = sq.n - sq.ql;
+  const int kblk0 = (int)kb, j0w = kblk0 + 32 * kw;
+
+  // This wave's keys as the A operand (row s, dims 16 kk + 8 hh ..).
+  typename M::x8 kr[KS];
+  {
+    const int row = min(j0w + s, sq.n - 1);
+    const int gr = granule_row(a.c, b, h, row >> 4);
+    const char* p = a.c.k + (long long)(max(gr, 0) + (row & 15)) * ROWB;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) kr[kk] = *reinterpret_cast<const typename M::x8*>(p + 32 * kk + 16 * hh);
+  }
+
+  // Column tiles holding a query at or after the block's first key.
+  const int it0 = (int)((long long)max(0, kblk0 - first) * G / 32);
+  const int nitems = (cols + 31) / 32 - it0;
+  const int qrow = (kWave * kw + lane) / CH;  // + 64 kSeedWaves / CH a load
+  float2 st_next = make_float2(0.0f, 0.0f);
+  auto issue = [&](int item, char* buf) {
+    if (item >= nitems) return;
+    const int col0 = 32 * (it0 + item);
+#pragma unroll
+    for (int k = 0; k < LPW; ++k) {
+      const int r = qrow + k * (kWave * kSeedWaves / CH);
+      const int c = min(col0 + r, cols - 1);  // columns past the last read it instead
+      load_lds((const char*)a.q + ((sq.q0 + c / G) * HQ + h * G + c % G) * (long long)ROWB + 16 * ((lane % CH) ^ (r % CH)),
+               (lds_char*)buf + ig * QTILE + kWave * 16 * (kw + kSeedWaves * k));
+    }
+    const int c = min(col0 + s, cols - 1);
+    st_next = ws.stat[(sq.q0 + c / G) * HQ + h * G + c % G];
+  };
+  float acc[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+  auto compute = [&](int item, const char* buf, float2 qs) {
+    if (item >= nitems || j0w >= sq.n) return;
+    const int c0 = 32 * (it0 + item);
+    if (first + min(c0 + 31, cols - 1) / G < j0w) return;  // every query precedes this wave's keys
+    const char* qt = buf + ig * QTILE;
+    mma_f32x16_t x;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk)
+      x = M::mma32(kr[kk], *reinterpret_cast<const typename M::x8*>(qt + 16 * Cfg::kslot(s, 2 * kk + hh)), x);
+    // A masked weight is left out, whatever its column's statistics hold.
+    const bool masked = first + c0 / G < j0w + 31 || c0 + 32 > cols;
+    const int lim = c0 + s < cols ? first + (c0 + s) / G - j0w - 4 * hh : -1;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p = hw_exp2((kCap ? logit2<true>(a, x[r]) : x[r] * a.scale_log2) - qs.x) * qs.y;
+      acc[r] += masked && 8 * (r >> 2) + (r & 3) > lim ? 0.0f : p;
+    }
+  };
+  issue(ig, buf0);
+  const int rounds = (nitems + kSeedGroups - 1) / kSeedGroups;
+  for (int x = 0; x < rounds; x += 2) {
+    wait_vmem();
+    __syncthreads();
+    float2 qs = st_next;
+    issue((x + 1) * kSeedGroups + ig, buf1);
+    compute(x * kSeedGroups + ig, buf0, qs);
+    if (x + 1 >= rounds) break;
+    wait_vmem();
+    __syncthreads();
+    qs = st_next;
+    issue((x + 2) * kSeedGroups + ig, buf0);
+    compute((x + 1) * kSeedGroups + ig, buf1, qs);
+  }
+  // Sum over the 32 columns: each exchange halves the keys a lane holds, until
+  // lane s holds key register s / 2.
+#pragma unroll
+  for (int half = 8; half >= 1; half /= 2) {
+    const bool up = (s & (2 * half)) != 0;
+#pragma unroll
+    for (int r = 0; r < half; ++r) {
+      const float mine = up ? acc[r + half] : acc[r];
+      const float give = up ? acc[r] : acc[r + half];
+      acc[r] = mine + __shfl_xor(give, 2 * half);
+    }
+  }
+  const float v = acc[0] + __shfl_xor(acc[0], 1);
+  const int r = s >> 1;
+  if ((s & 1) == 0) sums[ig][32 * kw + 8 * (r >> 2) + 4 * hh + (r & 3)] = v;
+  __syncthreads();
+  const int j = kblk0 + tid;
+  if (tid < kSeedKeys && j < sq.n) {
+    const int gr = granule_row(a.c, b, h, j >> 4);
+    if (gr >= 0) {
+      float* const sp = a.c.score + gr + (j & 15);
+      float t = sums[0][tid];
+#pragma unroll
+      for (int x = 1; x < kSeedGroups; ++x) t += sums[x][tid];
+      *sp = fmaf(a.gamma, *sp, t);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+struct Sizes {
+  int max_q, max_kv, R;
+  long long dec_grid, logit_rows;
+  long long items, slots, tiles;
+  size_t total;
+  DecWs dec;
+  TileWs tile;
+};
+
+// Grid sizes and the workspace's parts (their addresses from `ws` on).  The
+// bounds may be loose: no sequence that passes the checks has more queries
+// than there are query rows, or more rows than its table holds.
+bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ, int HK, int D, int64_t pool_rows, char* ws) {
+  const int G = HQ / HK;
+  z.max_q = (int)std::min<int64_t>(max_q, q_rows);
+  z.max_kv = (int)max_kv;
+  if (z.max_kv == 0) z.max_q = 0;
+  z.R = B <= kWave ? 1 : B <= 4 * kWave ? 4 : 16;
+  const long long steps = (z.max_kv + kDecStep - 1LL) / kDecStep * B;
+  if (steps * HK > 0x7fffffffLL) return false;
+  char* p = ws;
+  auto part = [&](size_t bytes) {
+    char* const at = p;
+    p += align_up(bytes, 256);
+    return at;
+  };
+  if (z.max_q <= 1) {
+    z.dec_grid = std::min(dec_blocks(steps * HK), steps * HK / kDecLeastSteps) + (long long)B * HK;
+    z.logit_rows = std::min(steps * kDecStep, pool_rows + (long long)B * kDecStep) * HK;
+    z.dec.part = (float*)part((size_t)z.dec_grid * dec_part(G, D) * 4);
+    z.dec.logit_rows = z.logit_rows;
+    z.dec.logit = (float*)part((size_t)z.logit_rows * dec_logits(G) * 4);
+  } else {
+    // Every sequence with queries rounds up to whole tiles.
+    z.tiles = q_rows * G / kTileCols + std::min<int64_t>(B, q_rows);
+    z.items = z.tiles + kRanges / HK + 1;
+    z.slots = z.max_kv <= kLeastKeys ? 0 : std::min<long long>(2LL * kRanges / HK + 2, z.tiles * std::min<long long>(kMaxSplit, (z.max_kv + kLeastKeys - 1) / kLeastKeys));
+    z.tile.max_items = (int)std::min(z.items, 0x7fffffffLL);
+    z.tile.max_slots = (int)z.slots;
+    z.tile.head = (PlanHead*)part(sizeof(PlanHead));
+    z.tile.keys = (int32_t*)part((size_t)B * 4);
+    z.tile.items = (PlanItem*)part((size_t)z.items * sizeof(PlanItem));
+    z.tile.splits = (PlanItem*)part((size_t)z.items * sizeof(PlanItem));
+    z.tile.stat = (float2*)part((size_t)q_rows * HQ * sizeof(float2));
+    z.tile.part_ml = (float2*)part((size_t)z.slots * HK * kTileCols * sizeof(float2));
+    z.tile.part_o = (float*)part((size_t)z.slots * HK * kTileCols * D * 4);
+    if (z.items * HK * kThreads > 0xffffffffLL) return false;
+  }
+  z.total = (size_t)(p - ws);
+  return true;
+}
+
+template <typename T, int D, bool kCap, int R>
+lethe_status launch_decode_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
+  hipLaunchKernelGGL((decode_kernel<T, D, kCap, R>), dim3((unsigned)z.dec_grid), dim3(kThreads), 0, s, a, z.dec);
+  if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
+  const unsigned y = a.gamma > 0.0f ? (unsigned)std::max(1LL, (z.max_kv + kFinRows - 1LL) / kFinRows) : 1u;
+  hipLaunchKernelGGL((finish_kernel<T, D, R>), dim3(a.c.B * a.c.HK, y), dim3(kThreads), 0, s, a, z.dec);
+  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+}
+
+template <typename T, int D, bool kCap>
+lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
+  if (z.max_q <= 1) {
+    if (z.R == 1) return launch_decode_form<T, D, kCap, 1>(a, z, s);
+    if (z.R == 4) return launch_decode_form<T, D, kCap, 4>(a, z, s);
+    return launch_decode_form<T, D, kCap, 16>(a, z, s);
+  }
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, z.tile);
+  if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
+  hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kThreads), 0, s, a, z.tile);
+  if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
+  if (z.slots > 0) {
+    const long long most = std::min(z.tiles, z.slots / 2 + 1);  // a cut tile has two slots at least
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)most, a.c.HK), dim3(kThreads), 0, s, a, z.tile);
+    if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
+  }
+  if (!(a.gamma > 0.0f)) return LETHE_OK;
+  const long long kblocks = (z.max_kv + kSeedKeys - 1LL) / kSeedKeys;
+  const unsigned y = (unsigned)std::min(kblocks, 32768LL), zz = (unsigned)((kblocks + y - 1) / y);
+  hipLaunchKernelGGL((seed_kernel<T, D, kCap>), dim3(a.c.B * a.c.HK, y, zz), dim3(kWave * kSeedWaves * kSeedGroups), 0, s,
+                     a, z.tile);
+  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+}
+
+template <typename T, int D>
+lethe_status launch_cap(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
+  return a.cap_log2 > 0.0f ? launch_form<T, D, true>(a, z, s) : launch_form<T, D, false>(a, z, s);
+}
+
+}  // namespace
+
+size_t paged_attn_ws_bytes(int64_t q_rows, int max_q, long long max_kv, int B, int HQ, int HK, int D, int64_t pool_rows) {
+  Sizes z{};
+  return sizes(z, q_rows, max_q, max_kv, B, HQ, HK, D, pool_rows, nullptr) ? std::max<size_t>(z.total, 256) : 0;
+}
+
+lethe_status launch_paged_attn(const PagedAttnArgs& args, lethe_dtype dt, int D, int64_t pool_rows, hipStream_t s) {
+  Sizes z{};
+  if (!sizes(z, args.q_rows, args.max_q, args.max_kv, args.c.B, args.c.HQ, args.c.HK, D, pool_rows, args.ws))
+    return LETHE_ERR_UNSUPPORTED;
+  PagedAttnArgs a = args;
+  a.max_q = z.max_q;
+  a.max_kv = z.max_kv;
+  if (dt == LETHE_BF16) return D == 128 ? launch_cap<__bf16, 128>(a, z, s) : launch_cap<__bf16, 64>(a, z, s);
+  return D == 128 ? launch_cap<_Float16, 128>(a, z, s) : launch_cap<_Float16, 64>(a, z, s);
+}
+
+}  // namespace lethe

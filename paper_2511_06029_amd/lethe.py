@@ -12,7 +12,8 @@ import os
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblethe.so")
 
 OK, ERR_INVALID, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4
-BF16, F32 = 0, 1
+BF16, F32, F16 = 0, 1, 2
+MAX_AXES = 4
 DEV_APPEND_OVERFLOW, DEV_INFEASIBLE, DEV_BAD_LAYOUT, DEV_HEAD_MISMATCH, DEV_WAIT_TIMEOUT = 1, 2, 4, 8, 16
 OP_DECODE, OP_SPARSITY, OP_SELECT, OP_COMPACT, OP_DECODE_FINAL, OP_COMPACT_PLAN = 0, 1, 2, 3, 4, 5
 
@@ -22,7 +23,9 @@ EXPORTED = ("lethe_workspace_bytes", "lethe_state_bytes", "lethe_decode_attn_sco
             "lethe_decode_attn_score_noalloc", "lethe_kv_compact_plan", "lethe_decode_attn_score_compact",
             "lethe_layer_sparsity", "lethe_rasr_select", "lethe_rasr_select_shared",
             "lethe_segmented_shrink", "lethe_kv_compact", "lethe_kv_compact_layers", "lethe_score_flush",
-            "lethe_prefill_attn_score", "lethe_prefill_workspace_bytes", "lethe_status_string")
+            "lethe_prefill_attn_score", "lethe_prefill_workspace_bytes", "lethe_paged_append",
+            "lethe_paged_attn_score", "lethe_paged_attn_workspace_bytes", "lethe_paged_evict",
+            "lethe_paged_evict_workspace_bytes", "lethe_status_string")
 
 
 class CCache(ctypes.Structure):
@@ -34,6 +37,26 @@ class CCache(ctypes.Structure):
         ("num_seqs", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
         ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("dev_status", ctypes.c_void_p), ("state", ctypes.c_void_p),
+    ]
+
+
+class CPagedCache(ctypes.Structure):
+    """Mirror of ``lethe_paged_cache``."""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("score", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+        ("len", ctypes.c_void_p), ("seen", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("num_layers", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("dev_status", ctypes.c_void_p),
+    ]
+
+
+class CRotary(ctypes.Structure):
+    """Mirror of ``lethe_rotary``."""
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p), ("axis_pos", ctypes.c_void_p), ("rot_dim", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * MAX_AXES), ("adjacent", ctypes.c_int32),
     ]
 
 
@@ -90,6 +113,19 @@ def load():
         lib.lethe_decode_attn_score_compact.argtypes = [pc, i32, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp,
                                                         vp, sz, vp, sz, vp]
         lib.lethe_decode_attn_score_compact.restype = ctypes.c_int
+        i64, pp = ctypes.c_int64, ctypes.POINTER(CPagedCache)
+        lib.lethe_paged_append.argtypes = [pp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i64, i32,
+                                           ctypes.POINTER(CRotary), vp, vp]
+        lib.lethe_paged_append.restype = ctypes.c_int
+        lib.lethe_paged_attn_score.argtypes = [pp, i32, vp, vp, vp, i64, i32, i32, ctypes.c_float, ctypes.c_float,
+                                               ctypes.c_float, vp, vp, sz, vp]
+        lib.lethe_paged_attn_score.restype = ctypes.c_int
+        lib.lethe_paged_attn_workspace_bytes.argtypes = [pp, i64, i32, i32]
+        lib.lethe_paged_attn_workspace_bytes.restype = sz
+        lib.lethe_paged_evict.argtypes = [pp, vp, i32, i32, vp, sz, vp]
+        lib.lethe_paged_evict.restype = ctypes.c_int
+        lib.lethe_paged_evict_workspace_bytes.argtypes = [pp]
+        lib.lethe_paged_evict_workspace_bytes.restype = sz
         lib.lethe_status_string.argtypes = [ctypes.c_int]
         lib.lethe_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -256,6 +292,155 @@ def decode_attn_score_compact(cache, layer, q, k_new, v_new, gamma, softmax_scal
                                                 plan.numel() * plan.element_size(), _p(ws),
                                                 ws.numel() * ws.element_size(), _stream(stream))
     _check("lethe_decode_attn_score_compact", st)
+
+
+def _row_stride(fn, t, heads, dim, dtype):
+    """Elements between the rows of a [rows][heads][dim] tensor whose heads lie side by side."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype:
+        raise LetheError(fn, ERR_INVALID)
+    if t.shape[0] and ((dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim)):
+        raise LetheError(fn, ERR_INVALID)
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def paged_append(cache, layer, q, k_new, v_new, q_start, q_len, max_q_len, rotary, q_out, stream=None):
+    """lethe_paged_append: rotate the new tokens' queries into q_out and their keys into the pages, with their
+    values; rows of q, k_new and v_new may be strided (parts of one projection).  q and q_out may both be None;
+    rotary None rotates nothing."""
+    fn = "lethe_paged_append"
+    rows = k_new.shape[0]
+    kd, vd = (_row_stride(fn, t, cache.HK, cache.D, cache.tdtype) for t in (k_new, v_new))
+    qd = 0 if q is None else _row_stride(fn, q, cache.HQ, cache.D, cache.tdtype)
+    if v_new.shape[0] != rows or (q is not None and q.shape[0] != rows):
+        raise LetheError(fn, ERR_INVALID)
+    if q_out is not None and (q_out.dtype != cache.tdtype or not q_out.is_contiguous() or
+                              tuple(q_out.shape) != (rows, cache.HQ, cache.D)):
+        raise LetheError(fn, ERR_INVALID)
+    if rotary is not None and rotary.rows != rows:
+        raise LetheError(fn, ERR_INVALID)
+    _check_batch(fn, cache, q_start, q_len)
+    st = load().lethe_paged_append(ctypes.byref(cache.c_struct()), int(layer), _p(q), qd, _p(k_new), kd, _p(v_new), vd,
+                                   _p(q_start), _p(q_len), int(rows), int(max_q_len),
+                                   None if rotary is None else ctypes.byref(rotary.c_struct()), _p(q_out),
+                                   _stream(stream))
+    _check(fn, st)
+
+
+def paged_attn_score(cache, layer, q, q_start, q_len, max_q_len, max_kv_len, gamma, softmax_scale, softcap, out, ws,
+                     stream=None):
+    """lethe_paged_attn_score: causal attention of the q_len newest rows of every sequence over its paged rows, with
+    the score update where gamma > 0; scores capped by softcap * tanh(x / softcap) where softcap > 0.  q and out:
+    [rows][H_Q][D] in the cache's type, contiguous; ws from cache.attn_workspace."""
+    fn = "lethe_paged_attn_score"
+    for t in (q, out):
+        if t.dtype != cache.tdtype or not t.is_contiguous() or tuple(t.shape) != (q.shape[0], cache.HQ, cache.D):
+            raise LetheError(fn, ERR_INVALID)
+    _check_batch(fn, cache, q_start, q_len)
+    st = load().lethe_paged_attn_score(ctypes.byref(cache.c_struct()), int(layer), _p(q), _p(q_start), _p(q_len),
+                                       int(q.shape[0]), int(max_q_len), int(max_kv_len), float(gamma),
+                                       float(softmax_scale), float(softcap), _p(out), _p(ws),
+                                       ws.numel() * ws.element_size(), _stream(stream))
+    _check(fn, st)
+
+
+def paged_evict(cache, budget, recent, sink, ws, stream=None):
+    """lethe_paged_evict: bring every segment to its budget (int32 [num_seqs][num_layers]); updates len.  ws from
+    cache.evict_workspace."""
+    fn = "lethe_paged_evict"
+    if str(budget.dtype) != "torch.int32" or not budget.is_contiguous() or tuple(budget.shape) != (cache.B, cache.L):
+        raise LetheError(fn, ERR_INVALID)
+    st = load().lethe_paged_evict(ctypes.byref(cache.c_struct()), _p(budget), int(recent), int(sink), _p(ws),
+                                  ws.numel() * ws.element_size(), _stream(stream))
+    _check(fn, st)
+
+
+def _check_batch(fn, cache, q_start, q_len):
+    for t, name in ((q_start, "torch.int64"), (q_len, "torch.int32")):
+        if str(t.dtype) != name or not t.is_contiguous() or t.numel() != cache.B:
+            raise LetheError(fn, ERR_INVALID)
+
+
+class Rotary:
+    """Rotary positions of a call of paged_append (``lethe_rotary``): inv_freq fp32 [rot_dim / 2], axis_pos int32
+    [axes][rows], sections the number of pairs of each axis; adjacent pairs elements 2j and 2j + 1 instead of j and
+    j + rot_dim / 2."""
+
+    def __init__(self, inv_freq, axis_pos, sections, adjacent=False):
+        if str(inv_freq.dtype) != "torch.float32" or not inv_freq.is_contiguous():
+            raise LetheError("Rotary", ERR_INVALID)
+        if str(axis_pos.dtype) != "torch.int32" or not axis_pos.is_contiguous() or axis_pos.dim() != 2:
+            raise LetheError("Rotary", ERR_INVALID)
+        if not 1 <= len(sections) <= MAX_AXES or axis_pos.shape[0] != len(sections):
+            raise LetheError("Rotary", ERR_INVALID)
+        self.inv_freq, self.axis_pos, self.rows = inv_freq, axis_pos, axis_pos.shape[1]
+        full = [int(x) for x in sections] + [0] * (MAX_AXES - len(sections))
+        self._c = CRotary(inv_freq.data_ptr(), axis_pos.data_ptr(), 2 * inv_freq.numel(), len(sections),
+                          (ctypes.c_int32 * MAX_AXES)(*full), int(bool(adjacent)))
+
+    def c_struct(self):
+        return self._c
+
+
+class LethePagedCache:
+    """A paged KV cache in the layout of include/lethe.h over tensors that the caller holds: k, v
+    [pages][H_KV][page_size][D], score fp32 and pos int32 [pages][H_KV][page_size], len and seen int32 [layers][seqs],
+    page_table int32 [layers][seqs][max_pages].  ``allocate`` makes them."""
+
+    def __init__(self, k, v, score, pos, len_, seen, page_table, num_q_heads):
+        import torch
+        self.torch = torch
+        self.num_pages, self.HK, self.page_size, self.D = (int(x) for x in k.shape)
+        self.L, self.B, self.max_pages = (int(x) for x in page_table.shape)
+        self.HQ = int(num_q_heads)
+        self.tdtype = k.dtype
+        codes = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+        rows = (self.num_pages, self.HK, self.page_size)
+        for t, dtype, shape in ((k, k.dtype, rows + (self.D,)), (v, k.dtype, rows + (self.D,)),
+                                (score, torch.float32, rows), (pos, torch.int32, rows),
+                                (len_, torch.int32, (self.L, self.B)), (seen, torch.int32, (self.L, self.B)),
+                                (page_table, torch.int32, (self.L, self.B, self.max_pages))):
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != k.device:
+                raise LetheError("LethePagedCache", ERR_INVALID)
+        if k.dtype not in codes:
+            raise LetheError("LethePagedCache", ERR_INVALID)
+        self.k, self.v, self.score, self.pos = k, v, score, pos
+        self.len, self.seen, self.page_table = len_, seen, page_table
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._c = CPagedCache(k.data_ptr(), v.data_ptr(), score.data_ptr(), pos.data_ptr(), len_.data_ptr(),
+                              seen.data_ptr(), page_table.data_ptr(), self.num_pages, self.page_size, self.max_pages,
+                              self.L, self.B, self.HQ, self.HK, self.D, codes[k.dtype], self.dev_status.data_ptr())
+        if self.evict_workspace_bytes() == 0:
+            raise LetheError("LethePagedCache", ERR_UNSUPPORTED)
+
+    @classmethod
+    def allocate(cls, num_layers, num_seqs, num_pages, page_size, max_pages, num_q_heads, num_kv_heads, head_dim,
+                 dtype="bf16", device="cuda"):
+        """An empty cache: no rows, no pages in any table (-1)."""
+        import torch
+        t = {"bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+        rows = (num_pages, num_kv_heads, page_size)
+        make = lambda shape, d: torch.zeros(shape, dtype=d, device=device)  # noqa: E731
+        return cls(make(rows + (head_dim,), t), make(rows + (head_dim,), t), make(rows, torch.float32),
+                   make(rows, torch.int32), make((num_layers, num_seqs), torch.int32),
+                   make((num_layers, num_seqs), torch.int32),
+                   torch.full((num_layers, num_seqs, max_pages), -1, dtype=torch.int32, device=device), num_q_heads)
+
+    def c_struct(self):
+        return self._c
+
+    def evict_workspace_bytes(self):
+        return int(load().lethe_paged_evict_workspace_bytes(ctypes.byref(self._c)))
+
+    def evict_workspace(self):
+        return self.torch.empty(self.evict_workspace_bytes(), dtype=self.torch.uint8, device=self.k.device)
+
+    def attn_workspace(self, q_rows, max_q_len, max_kv_len):
+        """Workspace of paged_attn_score for calls within these bounds."""
+        n = int(load().lethe_paged_attn_workspace_bytes(ctypes.byref(self._c), int(q_rows), int(max_q_len),
+                                                        int(max_kv_len)))
+        if n == 0:
+            raise LetheError("lethe_paged_attn_workspace_bytes", ERR_UNSUPPORTED)
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.k.device)
 
 
 class LetheCache:
