@@ -173,6 +173,7 @@ lethe_status lethe_paged_attn_score(const lethe_paged_cache* c, int32_t layer, c
   a.max_q = max_q_len;
   a.max_kv = most_rows(c, max_kv_len);
   a.G = c->num_q_heads / c->num_kv_heads;
+  a.g_magic = a.G > 1 ? (uint32_t)((0xffffffffULL + a.G) / a.G) : 0u;
   a.scale_log2 = scale * kLog2e;
   a.cap_in = softcap > 0.0f ? 2.0f * scale * kLog2e / softcap : 0.0f;
   a.cap_log2 = softcap * kLog2e;

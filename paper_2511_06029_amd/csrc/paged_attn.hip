@@ -65,15 +65,27 @@ __device__ inline int granule_row(const PagedView& c, int b, int h, int g) {
   return page_row(c, page, h) + (row & ((1 << c.page_shift) - 1));
 }
 
-// A raw product in base-2 logits: scaled, or scaled and capped,
-// cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)).
+// Base-2 logits are A v + B of a value v of the raw product x: x itself
+// (A = scale, B = 0), or, capped, 1 / (1 + exp(2 x / cap)), which falls as x
+// grows: cap tanh(x / cap) = cap - 2 cap v.
 template <bool kCap>
-__device__ inline float logit2(const PagedAttnArgs& a, float x) {
-  if constexpr (kCap)
-    return fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(1.0f + hw_exp2(x * a.cap_in)), a.cap_log2);
-  else
-    return x * a.scale_log2;
-}
+struct Logit {
+  float A, B, cap_in;
+  __device__ inline explicit Logit(const PagedAttnArgs& a)
+      : A(kCap ? -2.0f * a.cap_log2 : a.scale_log2), B(kCap ? a.cap_log2 : 0.0f), cap_in(a.cap_in) {}
+  __device__ inline float value(float x) const {
+    return kCap ? __builtin_amdgcn_rcpf(1.0f + hw_exp2(x * cap_in)) : x;
+  }
+  // The value of a masked logit, and the value of the larger logit.
+  static constexpr float kMasked = kCap ? INFINITY : -INFINITY;
+  static __device__ inline float larger(float u, float v) { return kCap ? fminf(u, v) : fmaxf(u, v); }
+  __device__ inline float logit(float v) const { return kCap ? fmaf(A, v, B) : A * v; }
+  // exp2(logit(v) - m) from shift = B - m.
+  __device__ inline float weight(float v, float shift) const { return hw_exp2(fmaf(A, v, shift)); }
+};
+
+// Query of column c, c / G (columns stay below 2^28: exact).
+__device__ inline int query_of(const PagedAttnArgs& a, int c) { return a.G == 1 ? c : (int)__umulhi((unsigned)c, a.g_magic); }
 
 __device__ inline float max_halves(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -85,7 +97,22 @@ __device__ inline void load_lds(const char* p, lds_char* dst) {
   __builtin_amdgcn_global_load_lds((global_cvoid*)p, (lds_void*)dst, 16, 0, 0);
 }
 
-__device__ inline void wait_vmem() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
+// Waits until at most N vector-memory operations are on their way (expcnt and
+// lgkmcnt left free).
+template <int N>
+__device__ inline void wait_vmem_but() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+__device__ inline void wait_vmem() { wait_vmem_but<0>(); }
+
+// A barrier without __syncthreads' wait for every load on its way: LDS reads
+// are done, and of the loads those that the caller has waited for.
+__device__ inline void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // ---------------------------------------------------------------------------
 // One query a sequence
@@ -263,6 +290,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   mma_f32x4_t o[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) o[nt] = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  const Logit<kCap> lg(a);
   const int lstride = dec_logits(G);
   float* const logit = a.gamma > 0.0f && dec_room(ws, ck) ? ws.logit + ck.row0 * lstride : nullptr;
 
@@ -295,7 +323,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) y = M::mma16(qb[kk], kr[t][kk], y);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = logit2<kCap>(a, y[r]);
+        for (int r = 0; r < 4; ++r) y[r] = lg.logit(lg.value(y[r]));
         const int row = base + 16 * t + s;
         if (4 * g4 < lstride && row < n) *reinterpret_cast<mma_f32x4_t*>(logit + (long long)row * lstride + 4 * g4) = y;
       }
@@ -313,7 +341,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        x[t][r] = logit2<kCap>(a, x[t][r]);
+        x[t][r] = lg.logit(lg.value(x[t][r]));
         if (dead && ((dead >> (16 * t + 4 * g4 + r)) & 1u)) x[t][r] = -INFINITY;
       }
     float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
@@ -458,11 +486,14 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs
 // ---------------------------------------------------------------------------
 // Longer queries
 // ---------------------------------------------------------------------------
-constexpr int kTileCols = 128;    // columns of a block
+constexpr int kTileWaves = 4;     // of a block, 32 columns each
+constexpr int kTileThreads = kWave * kTileWaves;
+constexpr int kTileCols = 32 * kTileWaves;
 constexpr int kKeyStep = 64;      // keys of a step
 constexpr int kLeastKeys = 512;   // of a key range
 constexpr int kRanges = 1024;     // blocks that the ranges aim at
 constexpr int kMaxSplit = 64;     // ranges of a tile
+constexpr float kLag = 8.0f;      // of a running maximum, base 2
 constexpr int kPlanThreads = 1024;
 constexpr int kBuckets = 1024;
 
@@ -482,8 +513,8 @@ struct TileWs {
   PlanItem* items;
   PlanItem* splits;
   float2* stat;      // [q_rows][HQ] max (base 2), 1 / sum
-  float2* part_ml;   // [slots][HK][128]
-  float* part_o;     // [slots][HK][128][D]
+  float2* part_ml;   // [slots][HK][kTileCols]
+  float* part_o;     // [slots][HK][kTileCols][D]
   int max_items, max_slots;
 };
 
@@ -580,26 +611,40 @@ struct TileCfg {
   // K tiles: piece c of row r at 16-byte slot r CH + (c ^ (r mod CH)), so the
   // rows that an operand read touches fall in different LDS banks.
   static constexpr int KTILE = kKeyStep * ROWB;
-  static constexpr int KPW = KTILE / (kThreads * 16);  // loads of a wave
+  static constexpr int KPW = KTILE / (kTileThreads * 16);  // loads of a wave
   static __device__ constexpr int kslot(int r, int c) { return r * CH + (c ^ (r % CH)); }
   // V tiles: load u (one wavefront) carries rows u + VLOADS j into block u.
   static constexpr int VLOADS = kKeyStep * CH / kWave;
-  static constexpr int VPW = VLOADS / kNumWaves;
+  static constexpr int VPW = VLOADS / kTileWaves;
   static constexpr int VBLK = kWave * 16 + 64;
   static constexpr int VTILE = VLOADS * VBLK;
   static __device__ constexpr int vaddr(int r, int c) { return (r % VLOADS) * VBLK + (r / VLOADS) * ROWB + c; }
 };
 
+// Order for the compiler's scheduler: N LDS reads next; one product and N
+// vector instructions next.
+template <int N>
+__device__ inline void sched_reads() {
+  __builtin_amdgcn_sched_group_barrier(0x100, N, 0);
+}
+template <int N>
+__device__ inline void sched_product() {
+  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+  __builtin_amdgcn_sched_group_barrier(0x402, N, 0);
+}
+
 template <typename T, int D, bool kCap>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(PagedAttnArgs a, TileWs ws) {
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(PagedAttnArgs a, TileWs ws) {
   using Cfg = TileCfg<D>;
   using M = Mma<T>;
   constexpr int KS = Cfg::KS, NT = Cfg::NT, ROWB = Cfg::ROWB, CH = Cfg::CH, STEP = kKeyStep;
   constexpr int KPW = Cfg::KPW, VPW = Cfg::VPW;
-  __shared__ __attribute__((aligned(16))) char ktile0[Cfg::KTILE];
-  __shared__ __attribute__((aligned(16))) char ktile1[Cfg::KTILE];
-  __shared__ __attribute__((aligned(16))) char vtile0[Cfg::VTILE];
-  __shared__ __attribute__((aligned(16))) char vtile1[Cfg::VTILE];
+  // Separate arrays, so that the compiler can tell a read of one tile from
+  // the direct loads that fill another.
+  __shared__ __attribute__((aligned(16))) char kt0[Cfg::KTILE];
+  __shared__ __attribute__((aligned(16))) char kt1[Cfg::KTILE];
+  __shared__ __attribute__((aligned(16))) char vt0[Cfg::VTILE];
+  __shared__ __attribute__((aligned(16))) char vt1[Cfg::VTILE];
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -625,22 +670,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   const int nsteps = (kend_blk - ks + STEP - 1) / STEP;
   const int own = kend > ks ? (kend - ks + STEP - 1) / STEP : 0;
   const int col = c0 + s;
-  const int pos = first + col / G;  // this lane's last key
-  const float sc = kCap ? 1.0f : a.scale_log2;
+  const int query = query_of(a, col);
+  const int pos = first + query;  // this lane's last key
+  const Logit<kCap> lg(a);
 
   // Queries as the B operand of S^T = K Q^T: lane (hh, s) holds
   // Q[column s][dims 16 kk + 8 hh ..].
   typename M::x8 qb[KS];
   {
-    const char* q = (const char*)a.q + ((sq.q0 + col / G) * HQ + h * G + col % G) * (long long)ROWB;
+    const char* q = (const char*)a.q + ((sq.q0 + query) * HQ + h * G + col - query * G) * (long long)ROWB;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk)
       qb[kk] = col < cols ? *reinterpret_cast<const typename M::x8*>(q + 32 * kk + 16 * hh) : mma_zero<T>();
   }
 
   // Granules of 16 steps at a time: lane l holds granule l of the window; even
-  // windows in ids[0], odd ones in ids[1], the next one asked for a window
-  // ahead.
+  // windows in ids0, odd ones in ids1, the next one asked for ahead.
   const int glast = (kend_blk - 1) >> 4;
   int ids0 = -1, ids1 = -1;
   bool bad = false;
@@ -663,15 +708,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const int last = kend_blk - 1 - j0;
 #pragma unroll
     for (int k = 0; k < KPW; ++k) {
-      constexpr int RPL = kThreads / CH;              // rows between a wave's loads
+      constexpr int RPL = kTileThreads / CH;          // rows between a wave's loads
       const int g = (RPL * k + kWave / CH * w) >> 4;  // uniform: a load stays in a granule
       if (last >= STEP - 1) {
         const char* p = a.c.k + (long long)max(granule(st, g), 0) * ROWB;
-        load_lds(p + (unsigned)((krow & 15) * ROWB + kpiece), kl + kWave * 16 * kNumWaves * k);
+        load_lds(p + (unsigned)((krow & 15) * ROWB + kpiece), kl + kWave * 16 * kTileWaves * k);
       } else {
         const int r = min(krow + RPL * k, last);
         const char* p = a.c.k + (long long)max(granule(st, min(g, last >> 4)), 0) * ROWB;
-        load_lds(p + (unsigned)((r & 15) * ROWB + kpiece), kl + kWave * 16 * kNumWaves * k);
+        load_lds(p + (unsigned)((r & 15) * ROWB + kpiece), kl + kWave * 16 * kTileWaves * k);
       }
     }
   };
@@ -687,19 +732,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       const int row = max(g < 2 ? (g == 0 ? i0 : i1) : (g == 2 ? i2 : i3), 0);
       const char* p = a.c.v + (long long)row * ROWB + (vrow & 15) * ROWB + 16 * (lane % CH);
 #pragma unroll
-      for (int k = 0; k < VPW; ++k) load_lds(p + k * kNumWaves * ROWB, vl + Cfg::VBLK * kNumWaves * k);
+      for (int k = 0; k < VPW; ++k) load_lds(p + k * kTileWaves * ROWB, vl + Cfg::VBLK * kTileWaves * k);
     } else {
 #pragma unroll
       for (int k = 0; k < VPW; ++k) {
-        const int r = min(vrow + kNumWaves * k, last);
+        const int r = min(vrow + kTileWaves * k, last);
         const int g = r >> 4;
         const int row = max(g < 2 ? (g == 0 ? i0 : i1) : (g == 2 ? i2 : i3), 0) + (r & 15);
-        load_lds(a.c.v + (long long)row * ROWB + 16 * (lane % CH), vl + Cfg::VBLK * kNumWaves * k);
+        load_lds(a.c.v + (long long)row * ROWB + 16 * (lane % CH), vl + Cfg::VBLK * kTileWaves * k);
       }
     }
   };
 
   float m = kNegBig, l = 0.0f, corr = 1.0f;
+  bool grown = false;
   mma_f32x16_t o[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -708,16 +754,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // S^T of a step: lane (hh, s), register r of sub-tile t: key j0 + 32 t +
   // 8 (r / 4) + 4 hh + r % 4, column s.
   mma_f32x16_t sa[2], sb[2];
-  auto clear = [&](mma_f32x16_t (&x)[2]) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[t][r] = 0.0f;
-  };
-  auto qk = [&](mma_f32x16_t (&x)[2], const char* kt, int kk) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-      x[t] = M::mma32(*reinterpret_cast<const typename M::x8*>(kt + 16 * Cfg::kslot(32 * t + s, 2 * kk + hh)), qb[kk], x[t]);
+  auto qk = [&](mma_f32x16_t& x, const char* kt, int t, int kk) {
+    x = M::mma32(*reinterpret_cast<const typename M::x8*>(kt + 16 * Cfg::kslot(32 * t + s, 2 * kk + hh)), qb[kk],
+                 kk == 0 ? mma_f32x16_t{} : x);
   };
   // Rows of step st on pages out of range, as bits of its granules.
   auto bad_granules = [&](int st) {
@@ -730,14 +769,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   };
   // A step is plain where every one of its rows counts for every column.
   auto plain = [&](int st) { return ks + st * STEP + STEP - 1 <= full && ks + (st + 1) * STEP <= kend && !bad; };
-  auto logits = [&](mma_f32x16_t (&x)[2], int st) {
+  auto col_max = [&](const mma_f32x16_t (&x)[2]) {
+    float mx = lg.larger(x[0][0], x[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = lg.larger(lg.larger(mx, x[0][r]), x[1][r]);
+    return mx;
+  };
+  auto capped = [&](mma_f32x16_t& x) {
     if constexpr (kCap) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[t][r] = logit2<true>(a, x[t][r]);
+      for (int r = 0; r < 16; ++r) x[r] = lg.value(x[r]);
     }
+  };
+  // Masks step st's logits, whose largest over all its rows has value mx, and
+  // moves the running maximum.
+  auto settle = [&](mma_f32x16_t (&x)[2], int st, float mx) {
     if (!plain(st)) {
+      asm volatile("");  // keeps the mask behind a branch
       const int j0 = ks + st * STEP;
       const int lim = min(pos, kend - 1) - j0 - 4 * hh;
       const unsigned bg = bad_granules(st);
@@ -745,19 +793,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (32 * t + 8 * (r >> 2) + (r & 3) > lim || ((bg >> (2 * t + (r >> 3))) & 1u)) x[t][r] = -INFINITY;
+          if (32 * t + 8 * (r >> 2) + (r & 3) > lim || ((bg >> (2 * t + (r >> 3))) & 1u)) x[t][r] = lg.kMasked;
+      mx = col_max(x);
     }
-    float mx = fmaxf(x[0][0], x[1][0]);
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, x[0][r]), x[1][r]);
-    const float mnew = fmaxf(m, max_halves(mx) * sc);
-    corr = hw_exp2(m - mnew);
-    m = mnew;
+    // The running maximum follows only where it would fall behind by more
+    // than kLag: weights then stay below 2^kLag, which the sums and both
+    // storage types hold with the same relative error, and the outputs are
+    // rescaled a few times a tile (following each maximum: in nearly every
+    // step, since one of 32 columns finds a new one).
+    const float top = max_halves(lg.logit(mx));
+    grown = __any(top > m + kLag);
+    if (grown) {
+      const float mnew = fmaxf(m, top);
+      corr = hw_exp2(m - mnew);
+      m = mnew;
+    }
   };
-  // Once the running maxima settle most steps leave every lane's correction at
-  // exactly 1; the wave then skips the rescale.
   auto rescale = [&]() {
-    if (__any(corr != 1.0f)) {
+    if (grown) {
       l *= corr;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -769,12 +822,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   // key 4 hh + j (j < 4) or 8 + 4 hh + j - 4.  They are rounded to the
   // storage type, as the output is; the sum is of the unrounded ones.
   float psum[2];
-  auto weights = [&](const mma_f32x16_t (&x)[2], int mm) {
-    typename M::x8 p;
+  auto half_weights = [&](const mma_f32x16_t (&x)[2], int mm, int half) {
+    typename M::x4 p;
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      const float pa = hw_exp2(fmaf(x[mm >> 1][8 * (mm & 1) + j], sc, -m));
-      const float pb = hw_exp2(fmaf(x[mm >> 1][8 * (mm & 1) + j + 1], sc, -m));
+    for (int j = 0; j < 4; j += 2) {
+      const float pa = lg.weight(x[mm >> 1][8 * (mm & 1) + 4 * half + j], lg.B - m);
+      const float pb = lg.weight(x[mm >> 1][8 * (mm & 1) + 4 * half + j + 1], lg.B - m);
       psum[0] += pa;
       psum[1] += pb;
       const typename M::x2 r = __builtin_convertvector((mma_f32x2_t{pa, pb}), typename M::x2);
@@ -782,6 +835,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
       p[j + 1] = r[1];
     }
     return p;
+  };
+  auto joined = [&](const typename M::x4& u, const typename M::x4& v) {
+    return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto weights = [&](const mma_f32x16_t (&x)[2], int mm) {
+    const typename M::x4 u = half_weights(x, mm, 0);
+    return joined(u, half_weights(x, mm, 1));
   };
   // V^T operand of keys 16 mm .. and dims 32 nt ..: lane i of a 16-lane group
   // points at row 4 hh + i / 4 (and 8 more), 4 columns from
@@ -793,31 +853,69 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const typename M::x4 a0 = M::read_tr(vt + Cfg::vaddr(vr, c)), a1 = M::read_tr(vt + Cfg::vaddr(vr + 8, c));
     return __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto pv = [&](const char* vtile, int mm, const typename M::x8& p) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) o[nt] = M::mma32(v_operand(vtile, mm, nt), p, o[nt]);
-  };
   // A plain step that is not this wave's last: weights and P V of step st,
-  // whose logits are in sx, interleaved with S^T of step st + 1 (K runs one
-  // tile ahead of V).
+  // whose logits are in sx, among S^T of step st + 1 (K runs one tile ahead of
+  // V).  In eight parts of four products each, S^T and P V in turn; a part's
+  // operands are read while the part before it runs.  The matrix and the
+  // vector units work side by side where a few vector instructions follow each
+  // product (a product of 32 cycles and six of them: 34 to 37; products in a
+  // row leave the vector units idle), so the weights are spread over the parts
+  // and the compiler is given the order.
   auto body = [&](int st, mma_f32x16_t (&sx)[2], mma_f32x16_t (&sn)[2], const char* knext, const char* vcur) {
+    constexpr int KQ = KS / 4;  // k-steps of a part
     rescale();
-    clear(sn);
     psum[0] = psum[1] = 0.0f;
-    typename M::x8 p = weights(sx, 0);
+    typename M::x8 kf[KQ][2], vf[NT];
+    auto read_k = [&](int part) {
 #pragma unroll
-    for (int kk = 0; kk < KS / 4; ++kk) qk(sn, knext, kk);
+      for (int kk = 0; kk < KQ; ++kk)
 #pragma unroll
-    for (int mm = 1; mm < 4; ++mm) {
-      const typename M::x8 pn = weights(sx, mm);
+        for (int t = 0; t < 2; ++t)
+          kf[kk][t] = *reinterpret_cast<const typename M::x8*>(knext + 16 * Cfg::kslot(32 * t + s, 2 * (KQ * part + kk) + hh));
+    };
+    read_k(0);
+    sched_reads<2 * KQ>();
+    typename M::x4 pa = half_weights(sx, 0, 0);
+    float mx = 0.0f;
 #pragma unroll
-      for (int kk = mm * KS / 4; kk < (mm + 1) * KS / 4; ++kk) qk(sn, knext, kk);
-      pv(vcur, mm - 1, p);
-      p = pn;
+    for (int mm = 0; mm < 4; ++mm) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) vf[nt] = v_operand(vcur, mm, nt);
+#pragma unroll
+      for (int kk = 0; kk < KQ; ++kk)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          sn[t] = M::mma32(kf[kk][t], qb[KQ * mm + kk], mm == 0 && kk == 0 ? mma_f32x16_t{} : sn[t]);
+      const typename M::x8 p = joined(pa, half_weights(sx, mm, 1));
+      sched_reads<2 * NT>();
+#pragma unroll
+      for (int i = 0; i < 2 * KQ; ++i) {
+        if (mm == 0)
+          sched_product<28 / (2 * KQ)>();
+        else
+          sched_product<16 / (2 * KQ)>();
+      }
+      if (mm < 3) {
+        read_k(mm + 1);
+        pa = half_weights(sx, mm + 1, 0);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) o[nt] = M::mma32(vf[nt], p, o[nt]);
+      if (mm < 3) {
+        sched_reads<2 * KQ>();
+#pragma unroll
+        for (int i = 0; i < NT; ++i) sched_product<16 / NT>();
+      }
     }
+    capped(sn[0]);
+    capped(sn[1]);
+    mx = col_max(sn);
     l += psum[0] + psum[1];
-    pv(vcur, 3, p);
-    logits(sn, st + 1);
+    // Sums and maximum stay among the products.
+    asm volatile("" : "+v"(l) : "v"(mx));
+#pragma unroll
+    for (int i = 0; i < NT; ++i) sched_product<24 / NT>();
+    settle(sn, st + 1, mx);
   };
   // Rows of a step that some columns do not attend must not meet them in a
   // product where they hold an infinity or NaN (0 times either is NaN).  Bits
@@ -895,65 +993,59 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   };
 
   // At step st, K of step st + 2 and V of step st + 1 are on their way into
-  // the buffers that step st - 1 has used.  Each wave waits for its own loads;
-  // the barrier makes every wave's visible and says that the buffers to fill
-  // have been read.
+  // the tiles that step st - 1 has read.  Each wave waits for its own loads;
+  // the barrier makes every wave's visible and says that those tiles are free.
   auto advance = [&](int st, char* kfill, char* vfill) {
     wait_vmem();
-    __syncthreads();
+    barrier_only();
+    issue_k(st + 2, kfill);
+    issue_v(st + 1, vfill);
     if ((st & 15) == 0 && st > 0) {
       if ((st >> 4) & 1)
         load_ids((st >> 4) + 1, ids0);
       else
         load_ids((st >> 4) + 1, ids1);
     }
-    issue_k(st + 2, kfill);
-    issue_v(st + 1, vfill);
   };
   load_ids(0, ids0);
   load_ids(1, ids1);
-  issue_k(0, ktile0);
-  issue_k(1, ktile1);
-  issue_v(0, vtile0);
+  issue_k(0, kt0);
+  issue_k(1, kt1);
+  issue_v(0, vt0);
   wait_vmem();
-  __syncthreads();
-  clear(sa);
-  if (own > 0) {
+  barrier_only();
+  auto alone = [&](int st, const char* kt) {
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) qk(sa, ktile0, kk);
-    logits(sa, 0);
-  }
-  // Steps before `lead` are plain and not the last.
-  int lead = min(own - 1, (min(full, kend - 1) + 1 - ks) / STEP);
-  if (bad) lead = 0;
+    for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) qk(sa[t], kt, t, kk);
+    capped(sa[0]);
+    capped(sa[1]);
+    settle(sa, st, col_max(sa));
+  };
+  if (own > 0) alone(0, kt0);
+  // Steps before `lead` are plain and not the last.  A page out of range
+  // further on ends them early.
+  const int lead = min(own - 1, (min(full, kend - 1) + 1 - ks) / STEP);
   int st = 0;
-  for (; st + 2 <= lead; st += 2) {
-    advance(st, ktile0, vtile1);
-    body(st, sa, sb, ktile1, vtile0);
-    advance(st + 1, ktile1, vtile0);
-    body(st + 1, sb, sa, ktile0, vtile1);
-    if (bad) break;  // a window further on has a page out of range
-  }
-  if (bad && st + 2 <= lead) {
-    st += 2;
-  } else if (st < lead) {
-    advance(st, ktile0, vtile1);
-    body(st, sa, sb, ktile1, vtile0);
+  while (st < lead && !bad) {
+    advance(st, kt0, vt1);
+    body(st, sa, sb, kt1, vt0);
+    if (++st >= lead || bad) break;
+    advance(st, kt1, vt0);
+    body(st, sb, sa, kt0, vt1);
     ++st;
+  }
+  if (st & 1) {
     sa[0] = sb[0];
     sa[1] = sb[1];
   }
   for (; st < own; ++st) {
-    advance(st, (st & 1) ? ktile1 : ktile0, (st & 1) ? vtile0 : vtile1);
-    careful(st, (st & 1) ? vtile1 : vtile0);
-    if (st + 1 < own) {
-      clear(sa);
-#pragma unroll
-      for (int kk = 0; kk < KS; ++kk) qk(sa, (st & 1) ? ktile0 : ktile1, kk);
-      logits(sa, st + 1);
-    }
+    advance(st, (st & 1) ? kt1 : kt0, (st & 1) ? vt0 : vt1);
+    careful(st, (st & 1) ? vt1 : vt0);
+    if (st + 1 < own) alone(st + 1, (st & 1) ? kt0 : kt1);
   }
-  for (; st < nsteps; ++st) advance(st, (st & 1) ? ktile1 : ktile0, (st & 1) ? vtile0 : vtile1);
+  for (; st < nsteps; ++st) advance(st, (st & 1) ? kt1 : kt0, (st & 1) ? vt0 : vt1);
   if (!active) return;
 
   // l is split over the two lane halves of a column; m is common.
@@ -971,7 +1063,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
   }
   if (col >= cols) return;
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no row at all: 0
-  const long long orow = (sq.q0 + col / G) * HQ + h * G + col % G;
+  const long long orow = (sq.q0 + query) * HQ + h * G + col - query * G;
   T* const out = (T*)a.out + orow * D;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -1029,120 +1121,179 @@ __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs 
   }
 }
 
-// Second pass, key-major.  A block is four waves of 32 keys each times two
+// Second pass, key-major.  A block is four waves of 32 NS keys each times two
 // groups of waves; group ig takes the column tiles ig, ig + 2, ... of 32
-// columns and keeps its own double-buffered query tile.
+// columns and keeps its own double-buffered query tile.  Bound by vector
+// instructions: a weight takes a multiply-add, an exp2 and a multiply-add
+// against 8 matrix-core cycles a lane, so the rest is kept small (64 keys a
+// wave share a tile's reads, addresses move by constants) and the products of
+// the next tile run among the weights of this one.
 constexpr int kSeedWaves = 4, kSeedGroups = 2;
-constexpr int kSeedKeys = 32 * kSeedWaves;
+constexpr int kSeedThreads = kWave * kSeedWaves * kSeedGroups;
+constexpr long long kSeedWide = 512;  // blocks of 64 keys a wave
 
-template <typename T, int D, bool kCap>
-__global__ __launch_bounds__(kWave* kSeedWaves* kSeedGroups) __attribute__((amdgpu_waves_per_eu(2))) void seed_kernel(
+template <typename T, int D, bool kCap, int NS>
+__global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS == 1 ? 4 : 2))) void seed_kernel(
     PagedAttnArgs a, TileWs ws) {
   using Cfg = TileCfg<D>;
   using M = Mma<T>;
   constexpr int KS = Cfg::KS, ROWB = Cfg::ROWB, CH = Cfg::CH;
+  constexpr int KEYS = 32 * NS * kSeedWaves;  // of a block
   constexpr int QTILE = 32 * ROWB;
   constexpr int LPW = QTILE / (kWave * 16) / kSeedWaves;  // loads of a wave
   static_assert(LPW >= 1, "a tile gives every wave of a group a load");
   __shared__ __attribute__((aligned(16))) char buf0[kSeedGroups * QTILE];
   __shared__ __attribute__((aligned(16))) char buf1[kSeedGroups * QTILE];
-  __shared__ float sums[kSeedGroups][kSeedKeys];
+  __shared__ float sums[kSeedGroups][KEYS];
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int kw = w % kSeedWaves, ig = w / kSeedWaves;
   const int hh = lane >> 5, s = lane & 31;
   const int b = blockIdx.x / a.c.HK, h = blockIdx.x % a.c.HK;
-  const long long kb = ((long long)blockIdx.y + (long long)gridDim.y * blockIdx.z) * kSeedKeys;
+  const long long kb = ((long long)blockIdx.y + (long long)gridDim.y * blockIdx.z) * KEYS;
   const AttnSeq sq = attn_seq(a, b);
   if (!sq.ok || sq.ql == 0 || kb >= sq.n) return;
   const int G = a.G, HQ = a.c.HQ, cols = sq.ql * G, first = sq.n - sq.ql;
-  const int kblk0 = (int)kb, j0w = kblk0 + 32 * kw;
+  const int kblk0 = (int)kb, j0w = kblk0 + 32 * NS * kw;
 
-  // This wave's keys as the A operand (row s, dims 16 kk + 8 hh ..).
-  typename M::x8 kr[KS];
-  {
-    const int row = min(j0w + s, sq.n - 1);
+  // This wave's keys as the A operand (row 32 t + s, dims 16 kk + 8 hh ..).
+  typename M::x8 kr[NS][KS];
+#pragma unroll
+  for (int t = 0; t < NS; ++t) {
+    const int row = min(j0w + 32 * t + s, sq.n - 1);
     const int gr = granule_row(a.c, b, h, row >> 4);
     const char* p = a.c.k + (long long)(max(gr, 0) + (row & 15)) * ROWB;
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) kr[kk] = *reinterpret_cast<const typename M::x8*>(p + 32 * kk + 16 * hh);
+    for (int kk = 0; kk < KS; ++kk) kr[t][kk] = *reinterpret_cast<const typename M::x8*>(p + 32 * kk + 16 * hh);
   }
 
-  // Column tiles holding a query at or after the block's first key.
+  // Column tiles holding a query at or after the block's first key.  A lane's
+  // place in its group's next tile, for each of its loads and for its
+  // column's statistics: row of q and head, and the head alone.
   const int it0 = (int)((long long)max(0, kblk0 - first) * G / 32);
   const int nitems = (cols + 31) / 32 - it0;
-  const int qrow = (kWave * kw + lane) / CH;  // + 64 kSeedWaves / CH a load
+  struct Place {
+    long long at;
+    int head;
+  };
+  auto place = [&](int c) {
+    const int qi = query_of(a, c);
+    return Place{(sq.q0 + qi) * HQ + h * G + c - qi * G, c - qi * G};
+  };
+  constexpr int kAdvance = 32 * kSeedGroups;
+  const int dq = kAdvance / G, dh = kAdvance % G;
+  auto move = [&](Place& x) {
+    x.at += dq * HQ + dh;
+    x.head += dh;
+    const bool wrap = x.head >= G;
+    x.at += wrap ? HQ - G : 0;
+    x.head -= wrap ? G : 0;
+  };
+  const int qrow = (kWave * kw + lane) / CH;                   // + 64 kSeedWaves / CH a load
+  const int piece = 16 * ((lane % CH) ^ (qrow % CH));          // the same for each: rows 16 or 32 apart
+  Place pl[LPW], ps = place(32 * (it0 + ig) + s);
+#pragma unroll
+  for (int k = 0; k < LPW; ++k) pl[k] = place(32 * (it0 + ig) + qrow + k * (kWave * kSeedWaves / CH));
+  int left = cols - 32 * (it0 + ig);  // columns from the group's next tile on
   float2 st_next = make_float2(0.0f, 0.0f);
-  auto issue = [&](int item, char* buf) {
-    if (item >= nitems) return;
-    const int col0 = 32 * (it0 + item);
+  auto issue = [&](char* buf) {
 #pragma unroll
     for (int k = 0; k < LPW; ++k) {
-      const int r = qrow + k * (kWave * kSeedWaves / CH);
-      const int c = min(col0 + r, cols - 1);  // columns past the last read it instead
-      load_lds((const char*)a.q + ((sq.q0 + c / G) * HQ + h * G + c % G) * (long long)ROWB + 16 * ((lane % CH) ^ (r % CH)),
-               (lds_char*)buf + ig * QTILE + kWave * 16 * (kw + kSeedWaves * k));
+      if (qrow + k * (kWave * kSeedWaves / CH) < left)
+        load_lds((const char*)a.q + pl[k].at * ROWB + piece, (lds_char*)buf + ig * QTILE + kWave * 16 * (kw + kSeedWaves * k));
+      move(pl[k]);
     }
-    const int c = min(col0 + s, cols - 1);
-    st_next = ws.stat[(sq.q0 + c / G) * HQ + h * G + c % G];
+    if (s < left) st_next = ws.stat[ps.at];
+    move(ps);
+    left -= kAdvance;
   };
-  float acc[16];
+  const Logit<kCap> lg(a);
+  float acc[NS][16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-  auto compute = [&](int item, const char* buf, float2 qs) {
-    if (item >= nitems || j0w >= sq.n) return;
-    const int c0 = 32 * (it0 + item);
-    if (first + min(c0 + 31, cols - 1) / G < j0w) return;  // every query precedes this wave's keys
+  for (int t = 0; t < NS; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
+  auto product = [&](mma_f32x16_t (&x)[NS], const char* buf) {
     const char* qt = buf + ig * QTILE;
-    mma_f32x16_t x;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+    for (int kk = 0; kk < KS; ++kk) {
+      const typename M::x8 q = *reinterpret_cast<const typename M::x8*>(qt + 16 * Cfg::kslot(s, 2 * kk + hh));
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk)
-      x = M::mma32(kr[kk], *reinterpret_cast<const typename M::x8*>(qt + 16 * Cfg::kslot(s, 2 * kk + hh)), x);
-    // A masked weight is left out, whatever its column's statistics hold.
-    const bool masked = first + c0 / G < j0w + 31 || c0 + 32 > cols;
-    const int lim = c0 + s < cols ? first + (c0 + s) / G - j0w - 4 * hh : -1;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float p = hw_exp2((kCap ? logit2<true>(a, x[r]) : x[r] * a.scale_log2) - qs.x) * qs.y;
-      acc[r] += masked && 8 * (r >> 2) + (r & 3) > lim ? 0.0f : p;
+      for (int t = 0; t < NS; ++t) x[t] = M::mma32(kr[t][kk], q, kk == 0 ? mma_f32x16_t{} : x[t]);
     }
   };
-  issue(ig, buf0);
+  // The weights of an item, whose products are in x, among the products of the
+  // next one, whose queries are in `buf`.  Columns past the last have whatever
+  // lies in their place; no product mixes columns.
+  auto step = [&](int item, mma_f32x16_t (&x)[NS], float2 qs, mma_f32x16_t (&xn)[NS], const char* buf) {
+    const int c0 = 32 * (it0 + item);
+    const float shift = lg.B - qs.x;
+    if (item < nitems && first + query_of(a, c0) >= j0w + 32 * NS - 1 && c0 + 32 <= cols) {
+      product(xn, buf);
+#pragma unroll
+      for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(lg.weight(lg.value(x[t][r]), shift), qs.y, acc[t][r]);
+    } else {
+      // A masked weight is left out, whatever its column's statistics hold.
+      const int lim = c0 + s < cols ? first + query_of(a, c0 + s) - j0w - 4 * hh : -1;
+#pragma unroll
+      for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = lg.weight(lg.value(x[t][r]), shift) * qs.y;
+          acc[t][r] += 32 * t + 8 * (r >> 2) + (r & 3) > lim ? 0.0f : p;
+        }
+      product(xn, buf);
+    }
+  };
+  // Round x: the products of item x + 1 need its queries (asked for two rounds
+  // ago); those of item x + 2 go where item x's were.
   const int rounds = (nitems + kSeedGroups - 1) / kSeedGroups;
+  float2 qs0, qs1;
+  mma_f32x16_t xa[NS], xb[NS];
+  issue(buf0);
+  qs0 = st_next;
+  issue(buf1);
+  qs1 = st_next;
+  wait_vmem();
+  barrier_only();
+  product(xa, buf0);
   for (int x = 0; x < rounds; x += 2) {
     wait_vmem();
-    __syncthreads();
-    float2 qs = st_next;
-    issue((x + 1) * kSeedGroups + ig, buf1);
-    compute(x * kSeedGroups + ig, buf0, qs);
+    barrier_only();
+    issue(buf0);
+    step(x * kSeedGroups + ig, xa, qs0, xb, buf1);
+    qs0 = st_next;
     if (x + 1 >= rounds) break;
     wait_vmem();
-    __syncthreads();
-    qs = st_next;
-    issue((x + 2) * kSeedGroups + ig, buf0);
-    compute((x + 1) * kSeedGroups + ig, buf1, qs);
+    barrier_only();
+    issue(buf1);
+    step((x + 1) * kSeedGroups + ig, xb, qs1, xa, buf0);
+    qs1 = st_next;
   }
   // Sum over the 32 columns: each exchange halves the keys a lane holds, until
   // lane s holds key register s / 2.
 #pragma unroll
-  for (int half = 8; half >= 1; half /= 2) {
-    const bool up = (s & (2 * half)) != 0;
+  for (int t = 0; t < NS; ++t) {
 #pragma unroll
-    for (int r = 0; r < half; ++r) {
-      const float mine = up ? acc[r + half] : acc[r];
-      const float give = up ? acc[r] : acc[r + half];
-      acc[r] = mine + __shfl_xor(give, 2 * half);
+    for (int half = 8; half >= 1; half /= 2) {
+      const bool up = (s & (2 * half)) != 0;
+#pragma unroll
+      for (int r = 0; r < half; ++r) {
+        const float mine = up ? acc[t][r + half] : acc[t][r];
+        const float give = up ? acc[t][r] : acc[t][r + half];
+        acc[t][r] = mine + __shfl_xor(give, 2 * half);
+      }
     }
+    const float v = acc[t][0] + __shfl_xor(acc[t][0], 1);
+    const int r = s >> 1;
+    if ((s & 1) == 0) sums[ig][32 * (NS * kw + t) + 8 * (r >> 2) + 4 * hh + (r & 3)] = v;
   }
-  const float v = acc[0] + __shfl_xor(acc[0], 1);
-  const int r = s >> 1;
-  if ((s & 1) == 0) sums[ig][32 * kw + 8 * (r >> 2) + 4 * hh + (r & 3)] = v;
   __syncthreads();
   const int j = kblk0 + tid;
-  if (tid < kSeedKeys && j < sq.n) {
+  if (tid < KEYS && j < sq.n) {
     const int gr = granule_row(a.c, b, h, j >> 4);
     if (gr >= 0) {
       float* const sp = a.c.score + gr + (j & 15);
@@ -1171,6 +1322,7 @@ struct Sizes {
 // than there are query rows, or more rows than its table holds.
 bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ, int HK, int D, int64_t pool_rows, char* ws) {
   const int G = HQ / HK;
+  if (q_rows > (1LL << 28) / G) return false;  // columns stay below 2^28
   z.max_q = (int)std::min<int64_t>(max_q, q_rows);
   z.max_kv = (int)max_kv;
   if (z.max_kv == 0) z.max_q = 0;
@@ -1203,7 +1355,7 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
     z.tile.stat = (float2*)part((size_t)q_rows * HQ * sizeof(float2));
     z.tile.part_ml = (float2*)part((size_t)z.slots * HK * kTileCols * sizeof(float2));
     z.tile.part_o = (float*)part((size_t)z.slots * HK * kTileCols * D * 4);
-    if (z.items * HK * kThreads > 0xffffffffLL) return false;
+    if (z.items * HK * kTileThreads > 0xffffffffLL) return false;
   }
   z.total = (size_t)(p - ws);
   return true;
@@ -1218,6 +1370,15 @@ lethe_status launch_decode_form(const PagedAttnArgs& a, const Sizes& z, hipStrea
   return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
 }
 
+template <typename T, int D, bool kCap, int NS>
+lethe_status launch_seed(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
+  constexpr int kKeys = 32 * NS * kSeedWaves;
+  const long long kblocks = (z.max_kv + kKeys - 1LL) / kKeys;
+  const unsigned y = (unsigned)std::min(kblocks, 32768LL), zz = (unsigned)((kblocks + y - 1) / y);
+  hipLaunchKernelGGL((seed_kernel<T, D, kCap, NS>), dim3(a.c.B * a.c.HK, y, zz), dim3(kSeedThreads), 0, s, a, z.tile);
+  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+}
+
 template <typename T, int D, bool kCap>
 lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
   if (z.max_q <= 1) {
@@ -1227,7 +1388,7 @@ lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) 
   }
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, z.tile);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kThreads), 0, s, a, z.tile);
+  hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kTileThreads), 0, s, a, z.tile);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   if (z.slots > 0) {
     const long long most = std::min(z.tiles, z.slots / 2 + 1);  // a cut tile has two slots at least
@@ -1235,11 +1396,9 @@ lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) 
     if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   }
   if (!(a.gamma > 0.0f)) return LETHE_OK;
-  const long long kblocks = (z.max_kv + kSeedKeys - 1LL) / kSeedKeys;
-  const unsigned y = (unsigned)std::min(kblocks, 32768LL), zz = (unsigned)((kblocks + y - 1) / y);
-  hipLaunchKernelGGL((seed_kernel<T, D, kCap>), dim3(a.c.B * a.c.HK, y, zz), dim3(kWave * kSeedWaves * kSeedGroups), 0, s,
-                     a, z.tile);
-  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+  // 64 keys a wave where their blocks fill the chip, else 32.
+  const long long wide = (z.max_kv + 64LL * kSeedWaves - 1) / (64 * kSeedWaves);
+  return wide * a.c.B * a.c.HK >= kSeedWide ? launch_seed<T, D, kCap, 2>(a, z, s) : launch_seed<T, D, kCap, 1>(a, z, s);
 }
 
 template <typename T, int D>

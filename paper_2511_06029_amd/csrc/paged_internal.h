@@ -50,6 +50,7 @@ struct PagedAttnArgs {
   const int32_t* q_len;
   int64_t q_rows;
   int32_t max_q, max_kv, G;
+  uint32_t g_magic;  // 2^32 / G, rounded up (G > 1)
   float scale_log2;  // softmax scale * log2(e)
   float cap_in;      // softcap > 0: 2 * scale * log2(e) / softcap
   float cap_log2;    // softcap * log2(e), 0 for none
