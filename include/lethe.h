@@ -504,8 +504,8 @@ lethe_status lethe_score_flush(const lethe_cache* cache, hipStream_t stream);
  *
  *  Conventions are those above (caller-owned device memory, asynchronous on
  *  `stream`, dev_status bits, no allocation, no state between calls).  k, v,
- *  and the q / k_new / v_new / q_out / out arguments (NULL with q_rows 0 is
- *  fine) must be 16-byte aligned, workspaces 256-byte aligned.
+ *  score, and the q / k_new / v_new / q_out / out arguments (NULL with q_rows
+ *  0 is fine) must be 16-byte aligned, workspaces 256-byte aligned.
  *  A page number outside [0, num_pages) sets LETHE_DEV_BAD_LAYOUT; what else
  *  it does is said at each call.  Sums are in a fixed order: the same call on
  *  the same inputs gives the same bits.

@@ -156,7 +156,7 @@ lethe_status lethe_paged_attn_score(const lethe_paged_cache* c, int32_t layer, c
   if (((uintptr_t)ws & 255) != 0) return LETHE_ERR_INVALID;
   if (max_kv_len < 0) return LETHE_ERR_INVALID;
   if (!(gamma >= 0.0f && gamma <= 1.0f)) return LETHE_ERR_INVALID;  // also rejects NaN
-  if (gamma > 0.0f && !c->score) return LETHE_ERR_INVALID;
+  if (gamma > 0.0f && (!c->score || !aligned16(c->score))) return LETHE_ERR_INVALID;
   if (isnan(softmax_scale) || isinf(softmax_scale)) return LETHE_ERR_INVALID;
   if (!(softcap >= 0.0f) || isinf(softcap)) return LETHE_ERR_INVALID;
   st = check_bounds(q_rows, max_q_len);

@@ -97,6 +97,11 @@ __device__ inline void load_lds(const char* p, lds_char* dst) {
   __builtin_amdgcn_global_load_lds((global_cvoid*)p, (lds_void*)dst, 16, 0, 0);
 }
 
+// The same for bytes that nothing else of the launch reads: they leave L2 early.
+__device__ inline void load_lds_nt(const char* p, lds_char* dst) {
+  __builtin_amdgcn_global_load_lds((global_cvoid*)p, (lds_void*)dst, 16, 0, 2);
+}
+
 // Waits until at most N vector-memory operations are on their way (expcnt and
 // lgkmcnt left free).
 template <int N>
@@ -122,7 +127,8 @@ constexpr int kDecMaxChunks = 64;   // of a segment
 constexpr int kDecChunkSteps = 14;  // steps of a chunk, where there are enough
 constexpr int kDecLeastSteps = 4;   // one a wavefront
 constexpr int kDecMinBlocks = 512, kDecMaxBlocks = 4096;
-constexpr int kFinRows = 1024;      // rows of a finishing block
+constexpr int kFinUnit = 4 * kThreads;  // rows that a finishing block takes at a time, four a thread
+constexpr long long kFinBlocks = 4096;  // about as many finishing blocks as there should be
 
 __host__ __device__ inline long long dec_blocks(long long steps) {
   const long long nb = steps / kDecChunkSteps;
@@ -130,12 +136,11 @@ __host__ __device__ inline long long dec_blocks(long long steps) {
 }
 // Floats of a chunk's partial: (max, sum) and output of every head.
 __host__ __device__ inline int dec_part(int G, int D) { return (G * (D + 2) + 31) / 32 * 32; }
-__host__ __device__ inline int dec_logits(int G) { return G <= 4 ? 4 : 8; }  // floats of a row
 
 struct DecChunk {
   int b, h, c, nch, n;
   int first;               // block index of the segment's chunk 0
-  long long row0;          // the segment's first row in the logits
+  long long row0;          // rows of the segments before it, rounded up to steps: its logits start at row0 G
   long long q0;
 };
 
@@ -267,23 +272,41 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     g1 = __builtin_amdgcn_readlane(ids, 2 * i + 1);
   };
   // Rows past the last one read that one instead; a granule out of range
-  // reads the pool's first rows.
+  // reads the pool's first rows.  Whole steps take two addresses for K (the
+  // granules', the same for every lane) and one for V.
   auto row_of = [&](int base, int r) {
     r = min(r, n - 1 - base);
     return (long long)(max(r < 16 ? g0 : g1, 0) + (r & 15)) * ROWB;
   };
   auto load_k = [&](int base) {
+    if (base + kDecStep <= n) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const char* p = a.c.k + row_of(base, 16 * t + s) + 16 * g4;
+      for (int t = 0; t < 2; ++t) {
+        const char* p = a.c.k + (long long)max(t ? g1 : g0, 0) * ROWB;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kr[t][kk] = *reinterpret_cast<const typename M::x8*>(p + 64 * kk);
+        for (int kk = 0; kk < KK; ++kk)
+          kr[t][kk] = *reinterpret_cast<const typename M::x8*>(p + (unsigned)(s * ROWB + 16 * g4) + 64 * kk);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const char* p = a.c.k + row_of(base, 16 * t + s) + 16 * g4;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kr[t][kk] = *reinterpret_cast<const typename M::x8*>(p + 64 * kk);
+      }
     }
   };
+  const int vrow = VLOADS * (lane / LPR);  // + u for load u; lanes of the upper half have granule 1
   auto load_v = [&](int base) {
+    if (base + kDecStep <= n) {
+      const char* p = a.c.v + (long long)(max(lane < kWave / 2 ? g0 : g1, 0) + (vrow & 15)) * ROWB + 16 * (lane % LPR);
 #pragma unroll
-    for (int u = 0; u < VLOADS; ++u)
-      load_lds(a.c.v + row_of(base, u + VLOADS * (lane / LPR)) + 16 * (lane % LPR), vb + u * Cfg::VBLK);
+      for (int u = 0; u < VLOADS; ++u) load_lds_nt(p + u * ROWB, vb + u * Cfg::VBLK);
+    } else {
+#pragma unroll
+      for (int u = 0; u < VLOADS; ++u)
+        load_lds(a.c.v + row_of(base, u + vrow) + 16 * (lane % LPR), vb + u * Cfg::VBLK);
+    }
   };
 
   float m = kNegBig, l = 0.0f;
@@ -291,8 +314,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) o[nt] = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   const Logit<kCap> lg(a);
-  const int lstride = dec_logits(G);
-  float* const logit = a.gamma > 0.0f && dec_room(ws, ck) ? ws.logit + ck.row0 * lstride : nullptr;
+  // Logits, [step][head][row of the step]: a step's lie side by side.
+  float* const logit =
+      a.gamma > 0.0f && dec_room(ws, ck) && s < G ? ws.logit + ck.row0 * G + s * kDecStep + 4 * g4 : nullptr;
 
   int step = first + w, i = 0;
   if (step < end) {
@@ -314,20 +338,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) x[t] = M::mma16(kr[t][kk], qb[kk], x[t]);
     }
-    if (logit) {
-      // The other orientation: lane (g4 < 2, s) gets heads 4 g4 .. + 3 of row
-      // 16 t + s, one 16-byte store.
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        mma_f32x4_t y = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) y = M::mma16(qb[kk], kr[t][kk], y);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = lg.logit(lg.value(y[r]));
-        const int row = base + 16 * t + s;
-        if (4 * g4 < lstride && row < n) *reinterpret_cast<mma_f32x4_t*>(logit + (long long)row * lstride + 4 * g4) = y;
-      }
-    }
     if (next < end) {
       if (++i == kWave / 2) {
         load_ids(next);
@@ -344,6 +354,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
         x[t][r] = lg.logit(lg.value(x[t][r]));
         if (dead && ((dead >> (16 * t + 4 * g4 + r)) & 1u)) x[t][r] = -INFINITY;
       }
+    if (logit) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) *reinterpret_cast<mma_f32x4_t*>(logit + (long long)base * G + 16 * t) = x[t];
+    }
     float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                      fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
     mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -366,17 +380,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
     // at row 4 g4 + s / 4 (and 16 more), column 16 nt + 4 (s % 4); its slots
     // j < 4 are rows 4 g4 + j, the others 16 + 4 g4 + j - 4, as p's.
     const int rsub = 4 * g4 + (s >> 2);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    auto operand = [&](int nt) {
       const int col = (16 * nt + 4 * (s & 3)) * 2;
       const typename M::x4 a0 = M::read_tr(vb + Cfg::vaddr(rsub, col)), a1 = M::read_tr(vb + Cfg::vaddr(rsub + 16, col));
-      typename M::x8 av = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-      if (dead) {
+      return __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    if (!dead) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) o[nt] = M::mma16(operand(nt), p, o[nt]);
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        typename M::x8 av = operand(nt);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if ((dead >> (16 * (j >> 2) + 4 * g4 + (j & 3))) & 1u) av[j] = (T)0.0f;
+        o[nt] = M::mma16(av, p, o[nt]);
       }
-      o[nt] = M::mma16(av, p, o[nt]);
     }
     if (next < end) {
       // The tile's reads are done (their results are in the products above).
@@ -419,18 +439,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   }
 }
 
-// blockIdx.x = segment, blockIdx.y = range of kFinRows rows.  Every block
-// joins the chunks' statistics; the first one of a segment the outputs too.
+// blockIdx.x = segment; blockIdx.y = 0: its output, y > 0: the scores of the
+// rows (y - 1) span ...  Every block joins the chunks' statistics.
 template <typename T, int D, int R>
-__global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs ws) {
+__global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs ws, int span) {
   constexpr int kMaxG = 8;
-  __shared__ float factor[kDecMaxChunks][kMaxG];  // what a chunk's output counts
+  __shared__ float factor[kMaxG][kDecMaxChunks];  // what a chunk's output counts
   __shared__ float2 stat[kMaxG];                  // max, 1 / sum
   const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
   DecChunk ck;
   if (!dec_chunk<R>(a, -1, blockIdx.x, ck)) return;
-  const long long r0 = (long long)blockIdx.y * kFinRows;
-  if (r0 >= ck.n) return;
+  const long long r0 = (blockIdx.y - 1LL) * span;
+  if (blockIdx.y > 0 && r0 >= ck.n) return;
   const int G = a.G, pstride = dec_part(G, D);
   const float* const part = ws.part + (long long)ck.first * pstride;
   for (int g = w; g < G; g += kNumWaves) {
@@ -440,45 +460,66 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs
     const float f = hw_exp2(ml.x - mm);
     const float sum = wave_sum(f * ml.y);
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // no row at all: 0
-    factor[lane][g] = f * inv;
+    factor[g][lane] = f * inv;
     if (lane == 0) stat[g] = make_float2(mm, inv);
   }
   __syncthreads();
-  if (r0 == 0) {
+  if (blockIdx.y == 0) {
     T* const out = (T*)a.out + (ck.q0 * a.c.HQ + (long long)ck.h * G) * D;
     for (int x = tid; x < G * D; x += kThreads) {
       const int g = x / D;
+      const float* const po = part + 2 * G + x;
       float sum = 0.0f;
-#pragma unroll 4
-      for (int c = 0; c < ck.nch; ++c) sum = fmaf(factor[c][g], part[(long long)c * pstride + 2 * G + x], sum);
+      for (int c0 = 0; c0 < ck.nch; c0 += 8) {
+        float v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = po[(long long)min(c0 + c, ck.nch - 1) * pstride];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum = fmaf(c0 + c < ck.nch ? factor[g][c0 + c] : 0.0f, v[c], sum);
+      }
       out[x] = (T)sum;
     }
+    return;
   }
-  if (!(a.gamma > 0.0f)) return;
   if (!dec_room(ws, ck)) {
     if (tid == 0) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
     return;
   }
-  const int ls = dec_logits(G);
-  const float* const logit = ws.logit + ck.row0 * ls;
+  const float* const logit = ws.logit + ck.row0 * G;
   const int mask = (1 << a.c.page_shift) - 1;
+  const int end = (int)min(r0 + span, (long long)ck.n);
+  // Four rows a thread: their scores lie side by side (a page holds whole
+  // granules of 16).
+  for (int r = (int)r0 + 4 * tid; r < end; r += kFinUnit) {
+    const int page = a.c.table[(long long)ck.b * a.c.max_pages + (r >> a.c.page_shift)];
+    mma_f32x4_t x[kMaxG];
 #pragma unroll
-  for (int i = 0; i < kFinRows / kThreads; ++i) {
-    const int r = (int)r0 + i * kThreads + tid;
-    if (r < ck.n) {
-      const int page = a.c.table[(long long)ck.b * a.c.max_pages + (r >> a.c.page_shift)];
-      if (page >= 0 && page < a.c.num_pages) {
-        float* const sp = a.c.score + page_row(a.c, page, ck.h) + (r & mask);
-        float acc = 0.0f;
-        for (int g0 = 0; g0 < G; g0 += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(logit + (long long)r * ls + g0);
-          const float xs[4] = {x.x, x.y, x.z, x.w};
+    for (int g = 0; g < kMaxG; ++g)
+      if (g < G) x[g] = *reinterpret_cast<const mma_f32x4_t*>(logit + (long long)(r / kDecStep * G + g) * kDecStep + r % kDecStep);
+    if (page < 0 || page >= a.c.num_pages) continue;
+    float* const sp = a.c.score + page_row(a.c, page, ck.h) + (r & mask);
+    mma_f32x4_t old;
+    if (r + 4 <= end) {
+      old = *reinterpret_cast<const mma_f32x4_t*>(sp);
+    } else {
 #pragma unroll
-          for (int g = 0; g < 4; ++g)
-            if (g0 + g < G) acc = fmaf(hw_exp2(xs[g] - stat[g0 + g].x), stat[g0 + g].y, acc);
-        }
-        *sp = fmaf(a.gamma, *sp, acc);
+      for (int i = 0; i < 4; ++i) old[i] = r + i < end ? sp[i] : 0.0f;
+    }
+    mma_f32x4_t sum = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int g = 0; g < kMaxG; ++g)
+      if (g < G) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = fmaf(hw_exp2(x[g][i] - stat[g].x), stat[g].y, sum[i]);
       }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) old[i] = fmaf(a.gamma, old[i], sum[i]);
+    if (r + 4 <= end) {
+      *reinterpret_cast<mma_f32x4_t*>(sp) = old;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r + i < end) sp[i] = old[i];
     }
   }
 }
@@ -1340,7 +1381,7 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
     z.logit_rows = std::min(steps * kDecStep, pool_rows + (long long)B * kDecStep) * HK;
     z.dec.part = (float*)part((size_t)z.dec_grid * dec_part(G, D) * 4);
     z.dec.logit_rows = z.logit_rows;
-    z.dec.logit = (float*)part((size_t)z.logit_rows * dec_logits(G) * 4);
+    z.dec.logit = (float*)part((size_t)z.logit_rows * G * 4);
   } else {
     // Every sequence with queries rounds up to whole tiles.
     z.tiles = q_rows * G / kTileCols + std::min<int64_t>(B, q_rows);
@@ -1365,8 +1406,13 @@ template <typename T, int D, bool kCap, int R>
 lethe_status launch_decode_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
   hipLaunchKernelGGL((decode_kernel<T, D, kCap, R>), dim3((unsigned)z.dec_grid), dim3(kThreads), 0, s, a, z.dec);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  const unsigned y = a.gamma > 0.0f ? (unsigned)std::max(1LL, (z.max_kv + kFinRows - 1LL) / kFinRows) : 1u;
-  hipLaunchKernelGGL((finish_kernel<T, D, R>), dim3(a.c.B * a.c.HK, y), dim3(kThreads), 0, s, a, z.dec);
+  // Rows of a finishing block: each repeats the map and the statistics.
+  const long long segs = (long long)a.c.B * a.c.HK;
+  const long long units = std::max(1LL, (z.max_kv + kFinUnit - 1LL) / kFinUnit);
+  const long long per = std::max(1LL, units * segs / kFinBlocks);
+  const unsigned y = 1u + (a.gamma > 0.0f ? (unsigned)((units + per - 1) / per) : 0u);
+  hipLaunchKernelGGL((finish_kernel<T, D, R>), dim3((unsigned)segs, y), dim3(kThreads), 0, s, a, z.dec,
+                     (int)std::min(per * kFinUnit, 0x40000000LL));
   return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
 }
 
