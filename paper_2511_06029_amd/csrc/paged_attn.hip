@@ -134,6 +134,16 @@ __host__ __device__ inline long long dec_blocks(long long steps) {
   const long long nb = steps / kDecChunkSteps;
   return nb < kDecMinBlocks ? kDecMinBlocks : nb > kDecMaxBlocks ? kDecMaxBlocks : nb;
 }
+// Steps of a chunk, of `all` steps over the call's segments, and chunks of a
+// segment.
+__host__ __device__ inline int dec_chunk_steps(long long all) {
+  const long long per = (all + dec_blocks(all) - 1) / dec_blocks(all);
+  return (int)(per < kDecLeastSteps ? kDecLeastSteps : per);
+}
+__host__ __device__ inline int dec_chunks(int steps, int per) {
+  const int nch = (steps + per - 1) / per;
+  return nch < kDecMaxChunks ? nch : kDecMaxChunks;
+}
 // Floats of a chunk's partial: (max, sum) and output of every head.
 __host__ __device__ inline int dec_part(int G, int D) { return (G * (D + 2) + 31) / 32 * 32; }
 
@@ -158,7 +168,7 @@ __device__ inline bool dec_chunk(const PagedAttnArgs& a, int idx, int seg, DecCh
     steps[r] = rows[r] = 0;
     if (b < a.c.B) {
       const AttnSeq s = attn_seq(a, b);
-      if (s.ok && s.ql > 0) {
+      if (s.ok && s.ql == 1) {
         rows[r] = s.n;
         steps[r] = (s.n + kDecStep - 1) / kDecStep;
       } else if (!s.ok && blockIdx.x == 0 && threadIdx.x < kWave) {
@@ -168,13 +178,12 @@ __device__ inline bool dec_chunk(const PagedAttnArgs& a, int idx, int seg, DecCh
     total += steps[r];
   }
   for (int o = kWave / 2; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  const long long all = (long long)total * a.c.HK;
-  const int per = (int)max((long long)kDecLeastSteps, (all + dec_blocks(all) - 1) / dec_blocks(all));
+  const int per = dec_chunk_steps((long long)total * a.c.HK);
   int blocks0 = 0;
   long long steps0 = 0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int nch = steps[r] == 0 ? 0 : min((steps[r] + per - 1) / per, kDecMaxChunks);
+    const int nch = dec_chunks(steps[r], per);
     const int incl = wave_incl_scan_i32(nch * a.c.HK);
     const int sincl = wave_incl_scan_i32(steps[r]);
     const int sum = __builtin_amdgcn_readlane(incl, kWave - 1);
@@ -225,25 +234,25 @@ __device__ inline bool dec_room(const DecWs& ws, const DecChunk& ck) {
   return ck.row0 + (ck.n + kDecStep - 1) / kDecStep * kDecStep <= ws.logit_rows;
 }
 
-template <typename T, int D, bool kCap, int R>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void decode_kernel(PagedAttnArgs a, DecWs ws) {
+constexpr int kMaxG = 8;
+
+// One chunk by a block of kThreads; its partial goes to slot `slot`.  tile(w):
+// LDS of wave w, DecCfg::VTILE bytes.
+template <typename T, int D, bool kCap, class Tile>
+__device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, const DecChunk& ck, long long slot,
+                                    const Tile& tile, float2 (&wave_ml)[kNumWaves][kMaxG]) {
   using Cfg = DecCfg<D>;
   using M = Mma<T>;
   constexpr int KK = Cfg::KK, NT = Cfg::NT, ROWB = Cfg::ROWB, LPR = Cfg::LPR, VLOADS = Cfg::VLOADS;
-  constexpr int kMaxG = 8;
-  __shared__ __attribute__((aligned(16))) char vtiles[kNumWaves * Cfg::VTILE];
-  __shared__ float2 wave_ml[kNumWaves][kMaxG];
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int g4 = lane >> 4, s = lane & 15;
-  DecChunk ck;
-  if (!dec_chunk<R>(a, blockIdx.x, -1, ck)) return;
   const int G = a.G;
   const int n = ck.n;
   const int steps = (n + kDecStep - 1) / kDecStep;
   const int first = (int)((long long)steps * ck.c / ck.nch), end = (int)((long long)steps * (ck.c + 1) / ck.nch);
-  lds_char* const vb = (lds_char*)vtiles + w * Cfg::VTILE;
+  lds_char* const vb = (lds_char*)tile(w);
 
   // Queries as the B operand of S^T = K Q^T: lane (g4, s) holds
   // Q[head s][dims 32 kk + 8 g4 ..], heads past G zero.
@@ -421,7 +430,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
       *(__attribute__((address_space(3))) mma_f32x4_t*)(vb + (s * D + 16 * nt + 4 * g4) * 4) = o[nt];
   }
   __syncthreads();
-  float* const part = ws.part + (long long)blockIdx.x * dec_part(G, D);
+  float* const part = ws.part + slot * dec_part(G, D);
   for (int x = tid; x < G * D; x += kThreads) {
     const int g = x / D;
     float mm = wave_ml[0][g].x;
@@ -431,7 +440,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
 #pragma unroll
     for (int v = 0; v < kNumWaves; ++v) {
       const float f = hw_exp2(wave_ml[v][g].x - mm);
-      sum = fmaf(f, *reinterpret_cast<const float*>(vtiles + v * Cfg::VTILE + x * 4), sum);
+      sum = fmaf(f, *reinterpret_cast<const float*>(tile(v) + x * 4), sum);
       lsum = fmaf(f, wave_ml[v][g].y, lsum);
     }
     part[2 * G + x] = sum;
@@ -439,18 +448,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) v
   }
 }
 
-// blockIdx.x = segment; blockIdx.y = 0: its output, y > 0: the scores of the
-// rows (y - 1) span ...  Every block joins the chunks' statistics.
+template <typename T, int D, bool kCap, int R>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void decode_kernel(PagedAttnArgs a, DecWs ws) {
+  __shared__ __attribute__((aligned(16))) char vtiles[kNumWaves * DecCfg<D>::VTILE];
+  __shared__ float2 wave_ml[kNumWaves][kMaxG];
+  DecChunk ck;
+  if (!dec_chunk<R>(a, blockIdx.x, -1, ck)) return;
+  decode_chunk<T, D, kCap>(a, ws, ck, blockIdx.x, [&](int w) { return vtiles + w * DecCfg<D>::VTILE; }, wave_ml);
+}
+
+// What is left of a segment with one query: y = 0: its output, y > 0: the
+// scores of its rows from (y - 1) span on.  Every block joins the chunks'
+// statistics.
 template <typename T, int D, int R>
-__global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs ws, int span) {
-  constexpr int kMaxG = 8;
+__device__ inline void finish_segment(const PagedAttnArgs& a, const DecWs& ws, int span, int seg, long long y) {
   __shared__ float factor[kMaxG][kDecMaxChunks];  // what a chunk's output counts
   __shared__ float2 stat[kMaxG];                  // max, 1 / sum
   const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
   DecChunk ck;
-  if (!dec_chunk<R>(a, -1, blockIdx.x, ck)) return;
-  const long long r0 = (blockIdx.y - 1LL) * span;
-  if (blockIdx.y > 0 && r0 >= ck.n) return;
+  if (!dec_chunk<R>(a, -1, seg, ck)) return;
+  const long long r0 = (y - 1) * span;
+  if (y > 0 && r0 >= ck.n) return;
   const int G = a.G, pstride = dec_part(G, D);
   const float* const part = ws.part + (long long)ck.first * pstride;
   for (int g = w; g < G; g += kNumWaves) {
@@ -464,7 +482,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs
     if (lane == 0) stat[g] = make_float2(mm, inv);
   }
   __syncthreads();
-  if (blockIdx.y == 0) {
+  if (y == 0) {
     T* const out = (T*)a.out + (ck.q0 * a.c.HQ + (long long)ck.h * G) * D;
     for (int x = tid; x < G * D; x += kThreads) {
       const int g = x / D;
@@ -524,6 +542,11 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs
   }
 }
 
+template <typename T, int D, int R>
+__global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs ws, int span) {
+  finish_segment<T, D, R>(a, ws, span, blockIdx.x, blockIdx.y);
+}
+
 // ---------------------------------------------------------------------------
 // Longer queries
 // ---------------------------------------------------------------------------
@@ -532,20 +555,27 @@ constexpr int kTileThreads = kWave * kTileWaves;
 constexpr int kTileCols = 32 * kTileWaves;
 constexpr int kKeyStep = 64;      // keys of a step
 constexpr int kLeastKeys = 512;   // of a key range
-constexpr int kRanges = 1024;     // blocks that the ranges aim at
+constexpr int kRanges = 256;      // blocks that the ranges aim at
 constexpr int kMaxSplit = 64;     // ranges of a tile
 constexpr float kLag = 8.0f;      // of a running maximum, base 2
 constexpr int kPlanThreads = 1024;
 constexpr int kBuckets = 1024;
 
 struct PlanHead {
-  int items, splits;  // entries of the two lists
+  int items, splits, seeds;  // entries of the lists
+  int wide;                  // seed blocks of kSeedWide keys instead of kSeedNarrow
 };
-// One tile and key range, or (splits) one tile with several ranges.
+// Keys of a seeding block; below this many wide ones the narrow ones are used.
+constexpr int kSeedWide = 256, kSeedNarrow = 64, kSeedFill = 512;
+constexpr int kSeedGrid = 1024;  // seeding blocks launched, at most
+// One tile and key range, or (splits) one tile with several ranges, or one
+// chunk of a sequence with one query.
+constexpr int kNoTile = -1, kChunkItem = -2;
 struct PlanItem {
   int b, tile;
-  int range;   // or, in the split list, how many
-  int slot;    // of its partial, -1: the only range
+  int range;   // in the split list, how many; of a chunk, its number and, from bit 8 on, how many the segment has
+  int slot;    // of its partial, -1: the only range; of a chunk, the chunks of one head before the sequence
+  int steps0;  // of a chunk, the steps of one head before the sequence
 };
 
 struct TileWs {
@@ -553,22 +583,64 @@ struct TileWs {
   int32_t* keys;     // [B] keys of a range
   PlanItem* items;
   PlanItem* splits;
+  int2* seeds;       // sequence and key block
   float2* stat;      // [q_rows][HQ] max (base 2), 1 / sum
   float2* part_ml;   // [slots][HK][kTileCols]
   float* part_o;     // [slots][HK][kTileCols][D]
-  int max_items, max_slots;
+  int max_items, max_slots, max_seeds;
 };
 
 __device__ inline int tile_count(int cols) { return (cols + kTileCols - 1) / kTileCols; }
 // One past the last key that columns up to `last` attend.
 __device__ inline int key_end(const AttnSeq& s, int last, int G) { return s.n - s.ql + min(last / G, s.ql - 1) + 1; }
 
+// Exclusive prefix sums of K values a thread and their totals, over a block of
+// kPlanThreads.
+template <int K>
+__device__ inline void scan_all(int (&v)[K], int (&total)[K], int (&tmp)[8][kPlanThreads / kWave]) {
+  const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
+  int own[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    own[k] = v[k];
+    v[k] = wave_incl_scan_i32(v[k]);
+    if (lane == kWave - 1) tmp[k][w] = v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    int before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kPlanThreads / kWave; ++i) {
+      const int x = tmp[k][i];
+      before += i < w ? x : 0;
+      all += x;
+    }
+    total[k] = all;
+    v[k] += before - own[k];
+  }
+  __syncthreads();
+}
+
+// Sum of a float over the block, the same for every thread.
+__device__ inline float sum_all(float v, float (&tmp)[kPlanThreads / kWave]) {
+  v = group_sum<kWave>(v);
+  if ((threadIdx.x & (kWave - 1)) == 0) tmp[threadIdx.x / kWave] = v;
+  __syncthreads();
+  float all = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPlanThreads / kWave; ++i) all += tmp[i];
+  __syncthreads();
+  return all;
+}
+
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, TileWs ws) {
-  __shared__ long long scan_tmp[kPlanThreads / kWave + 1];
-  __shared__ int item0[kPlanThreads];       // first item of a sequence
-  __shared__ int split0[kPlanThreads];      // its first entry in the split list
-  __shared__ int slot0[kPlanThreads];       // its first partial
-  __shared__ int keys_of[kPlanThreads];     // keys of a range
+  __shared__ int scan_tmp[8][kPlanThreads / kWave];
+  __shared__ float sum_tmp[kPlanThreads / kWave];
+  // By sequence: rows and queries, first entry of its in the three lists,
+  // first partial, steps before it (one query), keys of a range.
+  __shared__ int rows_of[kPlanThreads], queries_of[kPlanThreads], item0[kPlanThreads], split0[kPlanThreads];
+  __shared__ int seed0[kPlanThreads], slot0[kPlanThreads], steps0[kPlanThreads], keys_of[kPlanThreads];
   __shared__ int hist[kBuckets];
   const int tid = threadIdx.x;
   AttnSeq s{0, 0, 0, true};
@@ -577,70 +649,119 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
     atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
     s.n = s.ql = 0;
   }
-  const int tiles = tile_count(s.ql * a.G);
-  long long work;
-  block_excl_scan<kPlanThreads>((long long)tiles * a.c.HK * s.n, scan_tmp, &work);
-  const long long want = max((long long)kLeastKeys, (work + kRanges - 1) / kRanges);
-  const int ranges = tiles ? (int)min((long long)kMaxSplit, (s.n + want - 1) / want) : 1;
+  rows_of[tid] = s.n;
+  queries_of[tid] = s.ql;
+  const int tiles = s.ql > 1 ? tile_count(s.ql * a.G) : 0;
+  const int steps = s.ql == 1 ? (s.n + kDecStep - 1) / kDecStep : 0;
+  const int wide_seeds = s.ql > 1 ? (s.n + kSeedWide - 1) / kSeedWide : 0;
+  int v1[2] = {steps, wide_seeds}, t1[2];
+  scan_all<2>(v1, t1, scan_tmp);
+  steps0[tid] = v1[0];
+  const int chunks = dec_chunks(steps, dec_chunk_steps((long long)t1[0] * a.c.HK));
+  const float work = sum_all((float)tiles * (float)s.n, sum_tmp) * (float)a.c.HK;
+  // Ranges of like length, about kRanges blocks in all: one block a CU keeps it
+  // two thirds as busy as two do, and a tile that is not cut needs no joining.
+  const float want = fmaxf((float)kLeastKeys, work / (float)kRanges);
+  const int ranges = max(1, min(kMaxSplit, (int)((float)s.n / want + 0.5f)));
   const int keys = (int)((((long long)s.n + ranges - 1) / ranges + kKeyStep - 1) / kKeyStep * kKeyStep);
   if (tid < a.c.B) ws.keys[tid] = keys;
   keys_of[tid] = keys;
-  long long total, splits, slots;
-  item0[tid] = (int)block_excl_scan<kPlanThreads>((long long)tiles * ranges, scan_tmp, &total);
-  split0[tid] = (int)block_excl_scan<kPlanThreads>(ranges > 1 ? tiles : 0, scan_tmp, &splits);
-  slot0[tid] = (int)block_excl_scan<kPlanThreads>(ranges > 1 ? (long long)tiles * ranges : 0, scan_tmp, &slots);
+  const bool wide = (long long)t1[1] * a.c.HK >= kSeedFill;
+  const int seed_keys = wide ? kSeedWide : kSeedNarrow;
+  const int seed_blocks = !(a.gamma > 0.0f) || s.ql <= 1 ? 0 : (s.n + seed_keys - 1) / seed_keys;
+  int v2[5] = {tiles * ranges + chunks, ranges > 1 ? tiles : 0, ranges > 1 ? tiles * ranges : 0, chunks, seed_blocks}, t2[5];
+  scan_all<5>(v2, t2, scan_tmp);
+  const float count = sum_all((float)tiles * (float)ranges + (float)chunks, sum_tmp);  // also where t2[0] would not hold it
+  item0[tid] = v2[0];
+  split0[tid] = v2[1];
+  slot0[tid] = chunks ? v2[3] : v2[2];
+  seed0[tid] = v2[4];
   // More work than the bounds allow: rows of q that belong to two sequences.
-  const bool over = total > ws.max_items || slots > ws.max_slots;
-  const int items = over ? 0 : (int)total;
-  hist[tid] = 0;
+  const bool over = count > 1.5e9f || t2[0] > ws.max_items || t2[2] > ws.max_slots || t2[4] > ws.max_seeds;
+  const int items = over ? 0 : t2[0], seeds = over ? 0 : t2[4];
   if (tid == 0) {
     if (over) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
-    ws.head->items = items;
-    ws.head->splits = over ? 0 : (int)splits;
+    *ws.head = PlanHead{items, over ? 0 : t2[1], seeds, wide ? 1 : 0};
   }
   __syncthreads();
-  // Item i: its sequence by bisection, then tile and range; keys it works on.
-  auto item = [&](int i, PlanItem& it) {
-    int lo = 0, hi = a.c.B;  // item0[lo] <= i < item0[hi] (empty sequences share a start)
+  // The sequence that entry i of a list belongs to (empty ones share a start).
+  auto sequence = [&](const int (&first)[kPlanThreads], int i) {
+    int lo = 0, hi = a.c.B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (item0[mid] <= i)
+      if (first[mid] <= i)
         lo = mid;
       else
         hi = mid;
     }
-    const AttnSeq q = attn_seq(a, lo);
-    const int per = keys_of[lo];
-    const int nr = (int)(((lo + 1 < kPlanThreads ? item0[lo + 1] : items) - item0[lo]) / tile_count(q.ql * a.G));
-    it.b = lo;
-    it.tile = (i - item0[lo]) / nr;
-    it.range = (i - item0[lo]) % nr;
-    it.slot = nr > 1 ? slot0[lo] + i - item0[lo] : -1;
-    const int end = key_end(q, kTileCols * it.tile + kTileCols - 1, a.G);
+    return lo;
+  };
+  // Item i and the keys it works on.
+  auto item = [&](int i, PlanItem& it) {
+    const int b = sequence(item0, i);
+    const int n = rows_of[b], ql = queries_of[b];
+    const int mine = (b + 1 < kPlanThreads ? item0[b + 1] : items) - item0[b];
+    it.b = b;
+    if (ql == 1) {
+      it.tile = kChunkItem;
+      it.range = (i - item0[b]) | mine << 8;
+      it.slot = slot0[b];
+      it.steps0 = steps0[b];
+      return max(n / mine, 1);
+    }
+    const int per = keys_of[b];
+    const int nr = mine / tile_count(ql * a.G);
+    it.steps0 = 0;
+    it.tile = (i - item0[b]) / nr;
+    it.range = (i - item0[b]) % nr;
+    it.slot = nr > 1 ? slot0[b] + i - item0[b] : -1;
+    const int end = key_end(AttnSeq{n, ql, 0, true}, kTileCols * it.tile + kTileCols - 1, a.G);
     const long long from = (long long)it.range * per;
     if (it.range == 0 && nr > 1) {
-      const PlanItem sp{lo, it.tile, (int)((end + per - 1) / per), slot0[lo] + it.tile * nr};
-      ws.splits[split0[lo] + it.tile] = sp;
+      const PlanItem sp{b, it.tile, (int)((end + per - 1) / per), slot0[b] + it.tile * nr, 0};
+      ws.splits[split0[b] + it.tile] = sp;
     }
     return from >= end ? 0 : (int)(min((long long)end, from + per) - from);
   };
-  auto bucket = [&](int keyn) { return kBuckets - 1 - min(keyn / kKeyStep, kBuckets - 1); };
-  for (int i = tid; i < items; i += kPlanThreads) {
-    PlanItem it;
-    atomicAdd(&hist[bucket(item(i, it))], 1);
-  }
-  __syncthreads();
-  long long unused;
-  const int before = (int)block_excl_scan<kPlanThreads>(hist[tid], scan_tmp, &unused);
-  hist[tid] = before;
-  __syncthreads();
-  for (int i = tid; i < items; i += kPlanThreads) {
-    PlanItem it;
-    const int keyn = item(i, it);
-    const int at = atomicAdd(&hist[bucket(keyn)], 1);  // the order within a bucket does not matter
-    if (keyn == 0) it.tile = -1;
-    ws.items[at] = it;
-  }
+  // Key block i of the seeding pass and the column tiles it meets.
+  auto seed = [&](int i, int2& x) {
+    x.x = sequence(seed0, i);
+    x.y = i - seed0[x.x];
+    const int n = rows_of[x.x], ql = queries_of[x.x];
+    return (int)(((long long)ql * a.G + 31) / 32 - (long long)max(0, x.y * seed_keys - (n - ql)) * a.G / 32);
+  };
+  // A list's entries, longest first (the order within a bucket does not
+  // matter).  A thread's only entry is formed once.
+  auto emit = [&](int count, const auto& entry, const auto& store) {
+    hist[tid] = 0;
+    __syncthreads();
+    int bin = 0;
+    for (int i = tid; i < count; i += kPlanThreads) {
+      bin = kBuckets - 1 - min(entry(i), kBuckets - 1);
+      atomicAdd(&hist[bin], 1);
+    }
+    __syncthreads();
+    int v[1] = {hist[tid]}, unused[1];
+    scan_all<1>(v, unused, scan_tmp);
+    hist[tid] = v[0];
+    __syncthreads();
+    for (int i = tid; i < count; i += kPlanThreads) {
+      if (count > kPlanThreads) bin = kBuckets - 1 - min(entry(i), kBuckets - 1);
+      store(atomicAdd(&hist[bin], 1));
+    }
+    __syncthreads();
+  };
+  PlanItem it;
+  emit(
+      items, [&](int i) {
+        const int keyn = item(i, it);
+        if (keyn == 0) it.tile = kNoTile;
+        return (keyn + kKeyStep - 1) / kKeyStep;
+      },
+      [&](int at) { ws.items[at] = it; });
+  int2 sd;
+  emit(
+      seeds, [&](int i) { return seed(i, sd); }, [&](int at) { ws.seeds[at] = sd; });
 }
 
 template <int D>
@@ -675,7 +796,7 @@ __device__ inline void sched_product() {
 }
 
 template <typename T, int D, bool kCap>
-__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(PagedAttnArgs a, TileWs ws) {
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(PagedAttnArgs a, TileWs ws, DecWs dec) {
   using Cfg = TileCfg<D>;
   using M = Mma<T>;
   constexpr int KS = Cfg::KS, NT = Cfg::NT, ROWB = Cfg::ROWB, CH = Cfg::CH, STEP = kKeyStep;
@@ -695,9 +816,25 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
   const int at = blockIdx.x / a.c.HK;
   if (at >= ws.head->items) return;
   const PlanItem it = ws.items[at];
-  if (it.tile < 0) return;
+  if (it.tile == kNoTile) return;
   const int b = it.b, G = a.G, HQ = a.c.HQ;
   const AttnSeq sq = attn_seq(a, b);
+  if (it.tile == kChunkItem) {
+    __shared__ float2 wave_ml[kNumWaves][kMaxG];
+    DecChunk ck;
+    ck.b = b;
+    ck.h = h;
+    ck.c = it.range & 255;
+    ck.nch = it.range >> 8;
+    ck.n = sq.n;
+    ck.first = it.slot * a.c.HK + h * ck.nch;
+    ck.row0 = ((long long)it.steps0 * a.c.HK + (long long)h * ((sq.n + kDecStep - 1) / kDecStep)) * kDecStep;
+    ck.q0 = sq.q0;
+    static_assert(Cfg::KTILE >= DecCfg<D>::VTILE && kTileThreads == kThreads, "a wave's tile fits a K tile");
+    decode_chunk<T, D, kCap>(a, dec, ck, ck.first + ck.c,
+                             [&](int v) { return v & 2 ? (v & 1 ? vt1 : vt0) : (v & 1 ? kt1 : kt0); }, wave_ml);
+    return;
+  }
   const int cols = sq.ql * G, first = sq.n - sq.ql;
   const int ks = it.range * ws.keys[b];
   // Keys [ks, kend) of this wave and of the block; rows up to `full` are
@@ -1116,13 +1253,19 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
   if (hh == 0 && a.gamma > 0.0f) ws.stat[orow] = make_float2(m, inv);
 }
 
-// Tiles whose keys were cut: blockIdx.x = entry of the split list, .y = KV
-// head; four columns a wave at a time, 16 lanes each.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs ws) {
-  if ((int)blockIdx.x >= ws.head->splits) return;
-  const PlanItem it = ws.splits[blockIdx.x];
-  const int h = blockIdx.y, G = a.G;
+// Tiles whose keys were cut (the first `tiles` blocks: entry of the split list
+// and KV head; 16 columns at a time, 16 lanes each), then the segments with
+// one query.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs ws, DecWs dec, unsigned tiles, int span) {
+  if (blockIdx.x >= tiles) {
+    const unsigned segs = (unsigned)(a.c.B * a.c.HK), i = blockIdx.x - tiles;
+    finish_segment<T, D, R>(a, dec, span, (int)(i % segs), i / segs);
+    return;
+  }
+  const int entry = blockIdx.x / a.c.HK, h = blockIdx.x % a.c.HK, G = a.G;
+  if (entry >= ws.head->splits) return;
+  const PlanItem it = ws.splits[entry];
   const AttnSeq sq = attn_seq(a, it.b);
   constexpr int EL = D / 16;  // dims of a lane
   const int sub = threadIdx.x / 16, x = threadIdx.x % 16;
@@ -1162,41 +1305,35 @@ __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs 
   }
 }
 
-// Second pass, key-major.  A block is four waves of 32 NS keys each times two
-// groups of waves; group ig takes the column tiles ig, ig + 2, ... of 32
+// Second pass, key-major.  A block is KW waves of 32 NS keys each times IG
+// groups of waves; group ig takes the column tiles ig, ig + IG, ... of 32
 // columns and keeps its own double-buffered query tile.  Bound by vector
 // instructions: a weight takes a multiply-add, an exp2 and a multiply-add
 // against 8 matrix-core cycles a lane, so the rest is kept small (64 keys a
 // wave share a tile's reads, addresses move by constants) and the products of
-// the next tile run among the weights of this one.
-constexpr int kSeedWaves = 4, kSeedGroups = 2;
-constexpr int kSeedThreads = kWave * kSeedWaves * kSeedGroups;
-constexpr long long kSeedWide = 512;  // blocks of 64 keys a wave
+// the next tile run among the weights of this one.  Where the blocks of 256
+// keys do not fill the chip, 64 keys and four groups.
+constexpr int kSeedThreads = 512;
 
-template <typename T, int D, bool kCap, int NS>
-__global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS == 1 ? 4 : 2))) void seed_kernel(
-    PagedAttnArgs a, TileWs ws) {
+template <typename T, int D, bool kCap, int NS, int KW, int IG>
+__device__ inline void seed_block(const PagedAttnArgs& a, const TileWs& ws, int b, int h, int kblk0, char* const buf0,
+                                  char* const buf1, float* const sums) {
   using Cfg = TileCfg<D>;
   using M = Mma<T>;
   constexpr int KS = Cfg::KS, ROWB = Cfg::ROWB, CH = Cfg::CH;
-  constexpr int KEYS = 32 * NS * kSeedWaves;  // of a block
+  constexpr int KEYS = 32 * NS * KW;  // of a block
   constexpr int QTILE = 32 * ROWB;
-  constexpr int LPW = QTILE / (kWave * 16) / kSeedWaves;  // loads of a wave
+  constexpr int LPW = QTILE / (kWave * 16) / KW;  // loads of a wave
   static_assert(LPW >= 1, "a tile gives every wave of a group a load");
-  __shared__ __attribute__((aligned(16))) char buf0[kSeedGroups * QTILE];
-  __shared__ __attribute__((aligned(16))) char buf1[kSeedGroups * QTILE];
-  __shared__ float sums[kSeedGroups][KEYS];
+  static_assert(KW * IG * kWave == kSeedThreads, "every wave has keys and a group");
   const int tid = threadIdx.x;
   const int lane = tid & (kWave - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int kw = w % kSeedWaves, ig = w / kSeedWaves;
+  const int kw = w % KW, ig = w / KW;
   const int hh = lane >> 5, s = lane & 31;
-  const int b = blockIdx.x / a.c.HK, h = blockIdx.x % a.c.HK;
-  const long long kb = ((long long)blockIdx.y + (long long)gridDim.y * blockIdx.z) * KEYS;
   const AttnSeq sq = attn_seq(a, b);
-  if (!sq.ok || sq.ql == 0 || kb >= sq.n) return;
   const int G = a.G, HQ = a.c.HQ, cols = sq.ql * G, first = sq.n - sq.ql;
-  const int kblk0 = (int)kb, j0w = kblk0 + 32 * NS * kw;
+  const int j0w = kblk0 + 32 * NS * kw;
 
   // This wave's keys as the A operand (row 32 t + s, dims 16 kk + 8 hh ..).
   typename M::x8 kr[NS][KS];
@@ -1222,7 +1359,7 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
     const int qi = query_of(a, c);
     return Place{(sq.q0 + qi) * HQ + h * G + c - qi * G, c - qi * G};
   };
-  constexpr int kAdvance = 32 * kSeedGroups;
+  constexpr int kAdvance = 32 * IG;
   const int dq = kAdvance / G, dh = kAdvance % G;
   auto move = [&](Place& x) {
     x.at += dq * HQ + dh;
@@ -1231,18 +1368,18 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
     x.at += wrap ? HQ - G : 0;
     x.head -= wrap ? G : 0;
   };
-  const int qrow = (kWave * kw + lane) / CH;                   // + 64 kSeedWaves / CH a load
-  const int piece = 16 * ((lane % CH) ^ (qrow % CH));          // the same for each: rows 16 or 32 apart
+  const int qrow = (kWave * kw + lane) / CH;                   // + 64 KW / CH a load
   Place pl[LPW], ps = place(32 * (it0 + ig) + s);
 #pragma unroll
-  for (int k = 0; k < LPW; ++k) pl[k] = place(32 * (it0 + ig) + qrow + k * (kWave * kSeedWaves / CH));
+  for (int k = 0; k < LPW; ++k) pl[k] = place(32 * (it0 + ig) + qrow + k * (kWave * KW / CH));
   int left = cols - 32 * (it0 + ig);  // columns from the group's next tile on
   float2 st_next = make_float2(0.0f, 0.0f);
   auto issue = [&](char* buf) {
 #pragma unroll
     for (int k = 0; k < LPW; ++k) {
-      if (qrow + k * (kWave * kSeedWaves / CH) < left)
-        load_lds((const char*)a.q + pl[k].at * ROWB + piece, (lds_char*)buf + ig * QTILE + kWave * 16 * (kw + kSeedWaves * k));
+      const int r = qrow + k * (kWave * KW / CH);
+      if (r < left)
+        load_lds((const char*)a.q + pl[k].at * ROWB + 16 * ((lane % CH) ^ (r % CH)), (lds_char*)buf + ig * QTILE + kWave * 16 * (kw + KW * k));
       move(pl[k]);
     }
     if (s < left) st_next = ws.stat[ps.at];
@@ -1291,7 +1428,7 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
   };
   // Round x: the products of item x + 1 need its queries (asked for two rounds
   // ago); those of item x + 2 go where item x's were.
-  const int rounds = (nitems + kSeedGroups - 1) / kSeedGroups;
+  const int rounds = (nitems + IG - 1) / IG;
   float2 qs0, qs1;
   mma_f32x16_t xa[NS], xb[NS];
   issue(buf0);
@@ -1305,13 +1442,13 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
     wait_vmem();
     barrier_only();
     issue(buf0);
-    step(x * kSeedGroups + ig, xa, qs0, xb, buf1);
+    step(x * IG + ig, xa, qs0, xb, buf1);
     qs0 = st_next;
     if (x + 1 >= rounds) break;
     wait_vmem();
     barrier_only();
     issue(buf1);
-    step((x + 1) * kSeedGroups + ig, xb, qs1, xa, buf0);
+    step((x + 1) * IG + ig, xb, qs1, xa, buf0);
     qs1 = st_next;
   }
   // Sum over the 32 columns: each exchange halves the keys a lane holds, until
@@ -1330,7 +1467,7 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
     }
     const float v = acc[t][0] + __shfl_xor(acc[t][0], 1);
     const int r = s >> 1;
-    if ((s & 1) == 0) sums[ig][32 * (NS * kw + t) + 8 * (r >> 2) + 4 * hh + (r & 3)] = v;
+    if ((s & 1) == 0) sums[ig * KEYS + 32 * (NS * kw + t) + 8 * (r >> 2) + 4 * hh + (r & 3)] = v;
   }
   __syncthreads();
   const int j = kblk0 + tid;
@@ -1338,11 +1475,30 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
     const int gr = granule_row(a.c, b, h, j >> 4);
     if (gr >= 0) {
       float* const sp = a.c.score + gr + (j & 15);
-      float t = sums[0][tid];
+      float t = sums[tid];
 #pragma unroll
-      for (int x = 1; x < kSeedGroups; ++x) t += sums[x][tid];
+      for (int x = 1; x < IG; ++x) t += sums[x * KEYS + tid];
       *sp = fmaf(a.gamma, *sp, t);
     }
+  }
+}
+
+template <typename T, int D, bool kCap>
+__global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(2))) void seed_kernel(PagedAttnArgs a, TileWs ws) {
+  constexpr int QTILE = 32 * TileCfg<D>::ROWB;
+  __shared__ __attribute__((aligned(16))) char buf0[4 * QTILE];
+  __shared__ __attribute__((aligned(16))) char buf1[4 * QTILE];
+  __shared__ float sums[2 * kSeedWide];
+  static_assert(2 * kSeedWide >= 4 * kSeedNarrow, "both forms' sums fit");
+  const PlanHead head = *ws.head;
+  for (int i = blockIdx.x; i < head.seeds * a.c.HK; i += gridDim.x) {
+    const int2 x = ws.seeds[i / a.c.HK];
+    const int h = i % a.c.HK;
+    if (head.wide)
+      seed_block<T, D, kCap, 2, 4, 2>(a, ws, x.x, h, x.y * kSeedWide, buf0, buf1, sums);
+    else
+      seed_block<T, D, kCap, 1, 2, 4>(a, ws, x.x, h, x.y * kSeedNarrow, buf0, buf1, sums);
+    __syncthreads();  // the buffers are free
   }
 }
 
@@ -1351,7 +1507,7 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(NS
 // ---------------------------------------------------------------------------
 struct Sizes {
   int max_q, max_kv, R;
-  long long dec_grid, logit_rows;
+  long long dec_grid;
   long long items, slots, tiles;
   size_t total;
   DecWs dec;
@@ -1376,23 +1532,28 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
     p += align_up(bytes, 256);
     return at;
   };
-  if (z.max_q <= 1) {
-    z.dec_grid = std::min(dec_blocks(steps * HK), steps * HK / kDecLeastSteps) + (long long)B * HK;
-    z.logit_rows = std::min(steps * kDecStep, pool_rows + (long long)B * kDecStep) * HK;
-    z.dec.part = (float*)part((size_t)z.dec_grid * dec_part(G, D) * 4);
-    z.dec.logit_rows = z.logit_rows;
-    z.dec.logit = (float*)part((size_t)z.logit_rows * G * 4);
-  } else {
+  z.dec_grid = std::min(dec_blocks(steps * HK), steps * HK / kDecLeastSteps) + (long long)B * HK;
+  z.dec.logit_rows = std::min(steps * kDecStep, pool_rows + (long long)B * kDecStep) * HK;
+  z.dec.part = (float*)part((size_t)z.dec_grid * dec_part(G, D) * 4);
+  z.dec.logit = (float*)part((size_t)z.dec.logit_rows * G * 4);
+  if (z.max_q > 1) {
     // Every sequence with queries rounds up to whole tiles.
     z.tiles = q_rows * G / kTileCols + std::min<int64_t>(B, q_rows);
-    z.items = z.tiles + kRanges / HK + 1;
+    z.items = z.tiles + kRanges / HK + 1 + z.dec_grid / HK + 1;
     z.slots = z.max_kv <= kLeastKeys ? 0 : std::min<long long>(2LL * kRanges / HK + 2, z.tiles * std::min<long long>(kMaxSplit, (z.max_kv + kLeastKeys - 1) / kLeastKeys));
     z.tile.max_items = (int)std::min(z.items, 0x7fffffffLL);
     z.tile.max_slots = (int)z.slots;
+    // Key blocks of sequences with several queries; narrow ones only where the
+    // wide ones are fewer than kSeedFill, four to a wide one at most.
+    const long long wide = std::min<int64_t>(B, q_rows / 2) * ((z.max_kv + kSeedWide - 1LL) / kSeedWide);
+    const long long seeds = std::max(wide, std::min(4 * wide, 4LL * kSeedFill / HK + 4));
+    if (seeds * HK > 0x7fffffffLL) return false;
+    z.tile.max_seeds = (int)seeds;
     z.tile.head = (PlanHead*)part(sizeof(PlanHead));
     z.tile.keys = (int32_t*)part((size_t)B * 4);
     z.tile.items = (PlanItem*)part((size_t)z.items * sizeof(PlanItem));
     z.tile.splits = (PlanItem*)part((size_t)z.items * sizeof(PlanItem));
+    z.tile.seeds = (int2*)part((size_t)seeds * sizeof(int2));
     z.tile.stat = (float2*)part((size_t)q_rows * HQ * sizeof(float2));
     z.tile.part_ml = (float2*)part((size_t)z.slots * HK * kTileCols * sizeof(float2));
     z.tile.part_o = (float*)part((size_t)z.slots * HK * kTileCols * D * 4);
@@ -1402,54 +1563,52 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
   return true;
 }
 
+// Finishing blocks of a segment: one for its output, and with scores one for
+// every `span` rows (each repeats the map and the statistics).
+unsigned finish_blocks(const PagedAttnArgs& a, int& span) {
+  const long long units = std::max(1LL, (a.max_kv + kFinUnit - 1LL) / kFinUnit);
+  const long long per = std::max(1LL, units * a.c.B * a.c.HK / kFinBlocks);
+  span = (int)std::min(per * kFinUnit, 0x40000000LL);
+  return 1u + (a.gamma > 0.0f ? (unsigned)((units + per - 1) / per) : 0u);
+}
+
 template <typename T, int D, bool kCap, int R>
-lethe_status launch_decode_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
+lethe_status launch_one_query(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
   hipLaunchKernelGGL((decode_kernel<T, D, kCap, R>), dim3((unsigned)z.dec_grid), dim3(kThreads), 0, s, a, z.dec);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  // Rows of a finishing block: each repeats the map and the statistics.
-  const long long segs = (long long)a.c.B * a.c.HK;
-  const long long units = std::max(1LL, (z.max_kv + kFinUnit - 1LL) / kFinUnit);
-  const long long per = std::max(1LL, units * segs / kFinBlocks);
-  const unsigned y = 1u + (a.gamma > 0.0f ? (unsigned)((units + per - 1) / per) : 0u);
-  hipLaunchKernelGGL((finish_kernel<T, D, R>), dim3((unsigned)segs, y), dim3(kThreads), 0, s, a, z.dec,
-                     (int)std::min(per * kFinUnit, 0x40000000LL));
+  int span;
+  const unsigned y = finish_blocks(a, span);
+  hipLaunchKernelGGL((finish_kernel<T, D, R>), dim3(a.c.B * a.c.HK, y), dim3(kThreads), 0, s, a, z.dec, span);
   return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
 }
 
-template <typename T, int D, bool kCap, int NS>
-lethe_status launch_seed(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
-  constexpr int kKeys = 32 * NS * kSeedWaves;
-  const long long kblocks = (z.max_kv + kKeys - 1LL) / kKeys;
-  const unsigned y = (unsigned)std::min(kblocks, 32768LL), zz = (unsigned)((kblocks + y - 1) / y);
-  hipLaunchKernelGGL((seed_kernel<T, D, kCap, NS>), dim3(a.c.B * a.c.HK, y, zz), dim3(kSeedThreads), 0, s, a, z.tile);
-  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
-}
-
-template <typename T, int D, bool kCap>
+template <typename T, int D, bool kCap, int R>
 lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
-  if (z.max_q <= 1) {
-    if (z.R == 1) return launch_decode_form<T, D, kCap, 1>(a, z, s);
-    if (z.R == 4) return launch_decode_form<T, D, kCap, 4>(a, z, s);
-    return launch_decode_form<T, D, kCap, 16>(a, z, s);
-  }
+  if (z.max_q <= 1) return launch_one_query<T, D, kCap, R>(a, z, s);
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, z.tile);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kTileThreads), 0, s, a, z.tile);
+  hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kTileThreads), 0, s, a, z.tile,
+                     z.dec);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  if (z.slots > 0) {
-    const long long most = std::min(z.tiles, z.slots / 2 + 1);  // a cut tile has two slots at least
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)most, a.c.HK), dim3(kThreads), 0, s, a, z.tile);
-    if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  }
+  // A cut tile has two slots at least.
+  int span;
+  const unsigned y = finish_blocks(a, span);
+  const unsigned tiles = (unsigned)(std::min(z.tiles, z.slots / 2) * a.c.HK);
+  hipLaunchKernelGGL((join_kernel<T, D, R>), dim3(tiles + (unsigned)(a.c.B * a.c.HK) * y), dim3(kThreads), 0, s, a, z.tile,
+                     z.dec, tiles, span);
+  if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   if (!(a.gamma > 0.0f)) return LETHE_OK;
-  // 64 keys a wave where their blocks fill the chip, else 32.
-  const long long wide = (z.max_kv + 64LL * kSeedWaves - 1) / (64 * kSeedWaves);
-  return wide * a.c.B * a.c.HK >= kSeedWide ? launch_seed<T, D, kCap, 2>(a, z, s) : launch_seed<T, D, kCap, 1>(a, z, s);
+  const unsigned blocks = (unsigned)std::min<long long>((long long)z.tile.max_seeds * a.c.HK, kSeedGrid);
+  hipLaunchKernelGGL((seed_kernel<T, D, kCap>), dim3(blocks), dim3(kSeedThreads), 0, s, a, z.tile);
+  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
 }
 
 template <typename T, int D>
 lethe_status launch_cap(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
-  return a.cap_log2 > 0.0f ? launch_form<T, D, true>(a, z, s) : launch_form<T, D, false>(a, z, s);
+  const bool cap = a.cap_log2 > 0.0f;
+  if (z.R == 1) return cap ? launch_form<T, D, true, 1>(a, z, s) : launch_form<T, D, false, 1>(a, z, s);
+  if (z.R == 4) return cap ? launch_form<T, D, true, 4>(a, z, s) : launch_form<T, D, false, 4>(a, z, s);
+  return cap ? launch_form<T, D, true, 16>(a, z, s) : launch_form<T, D, false, 16>(a, z, s);
 }
 
 }  // namespace
