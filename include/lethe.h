@@ -640,16 +640,19 @@ size_t lethe_paged_attn_workspace_bytes(const lethe_paged_cache* cache, int64_t 
  * Only rows whose place lies beyond the budget move (order-preserving
  * compaction moves every row after the first evicted one).
  *
- *  budget int32 [num_seqs][num_layers]; recent, sink >= 0.
+ *  budget int32 [num_seqs][num_layers]; recent, sink >= 0.  max_kv_len: host
+ *  upper bound of len (it chooses how many threads rank a segment; may be
+ *  loose).
  *  ws  lethe_paged_evict_workspace_bytes(cache) bytes.
- * A sequence with len out of range or a page out of range among its live rows
+ * A sequence with len or seen out of range (len above the bound or the table,
+ * seen below len) or a page out of range among its live rows
  * sets LETHE_DEV_BAD_LAYOUT and is left alone in that layer.  The tokens of a
  * segment's rows are distinct (appending makes them so).  Errors:
  * LETHE_ERR_INVALID, LETHE_ERR_UNSUPPORTED, LETHE_ERR_WORKSPACE,
  * LETHE_ERR_HIP.
  */
 lethe_status lethe_paged_evict(const lethe_paged_cache* cache, const int32_t* budget, int32_t recent, int32_t sink,
-                               void* ws, size_t ws_bytes, hipStream_t stream);
+                               int32_t max_kv_len, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Workspace bytes of lethe_paged_evict; 0 for an invalid description. */
 size_t lethe_paged_evict_workspace_bytes(const lethe_paged_cache* cache);

@@ -188,10 +188,11 @@ size_t lethe_paged_evict_workspace_bytes(const lethe_paged_cache* c) {
 }
 
 lethe_status lethe_paged_evict(const lethe_paged_cache* c, const int32_t* budget, int32_t recent, int32_t sink,
-                               void* ws, size_t ws_bytes, hipStream_t stream) {
+                               int32_t max_kv_len, void* ws, size_t ws_bytes, hipStream_t stream) {
   const lethe_status st = check_cache(c);
   if (st != LETHE_OK) return st;
-  if (!c->score || !c->pos || !c->seen || !budget || recent < 0 || sink < 0) return LETHE_ERR_INVALID;
+  if (!c->score || !c->pos || !c->seen || !budget || recent < 0 || sink < 0 || max_kv_len < 0)
+    return LETHE_ERR_INVALID;
   if (!ws || ((uintptr_t)ws & 255) != 0) return LETHE_ERR_INVALID;
   if (ws_bytes < evict_ws_bytes(c)) return LETHE_ERR_WORKSPACE;
   PagedEvictArgs a;
@@ -201,6 +202,7 @@ lethe_status lethe_paged_evict(const lethe_paged_cache* c, const int32_t* budget
   a.budget = budget;
   a.recent = recent;
   a.sink = sink;
+  a.max_kv = most_rows(c, max_kv_len);
   a.count = (int32_t*)ws;
   a.moves = (int2*)((char*)ws + evict_count_bytes(c));
   return launch_paged_evict(a, stream);

@@ -24,9 +24,7 @@ namespace lethe {
 
 namespace {
 
-constexpr int kEvRegs = 32;   // rows of a thread held in registers
 constexpr int kEvUnit = 8;    // rows whose loads leave together
-constexpr int kEvPages = 2048;  // table entries held in shared memory: 32 rows of 1024 threads on pages of 16
 
 // One (layer, sequence) of an eviction.
 struct EvSeq {
@@ -45,17 +43,17 @@ __device__ inline EvSeq ev_seq(const PagedEvictArgs& a, int lb) {
   return s;
 }
 
-template <int NT>
+template <int NT, int REGS>
 struct EvShared : RadixShared {
-  int pages[kEvPages];
-  int count[2][kEvRegs * (NT / kWave)];  // evicted / kept rows of a wave's 64, then their sums before it
+  int pages[NT * REGS / 16];
+  int count[2][REGS * (NT / kWave)];  // evicted / kept rows of a wave's 64, then their sums before it
   uint32_t red[2][NT / kWave];
   long long scan_tmp[NT / kWave + 1];
   int total[2];
 };
 
-template <int NT>
-__device__ inline uint2 block_sum2(uint32_t x, uint32_t y, EvShared<NT>& sh) {
+template <int NT, int REGS>
+__device__ inline uint2 block_sum2(uint32_t x, uint32_t y, EvShared<NT, REGS>& sh) {
   for (int o = kWave / 2; o > 0; o >>= 1) {
     x += (uint32_t)__shfl_xor(x, o);
     y += (uint32_t)__shfl_xor(y, o);
@@ -75,22 +73,22 @@ __device__ inline uint2 block_sum2(uint32_t x, uint32_t y, EvShared<NT>& sh) {
   return t;
 }
 
-// The lists of a segment with k < n whose pages are valid.  kRegs: n <=
-// kEvRegs * NT, keys and tokens in registers and the table in shared memory;
-// otherwise every pass reads them again.
-template <int NT, bool kRegs>
-__device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, EvShared<NT>& sh, int32_t* count) {
+// The lists of a segment with k < n whose pages are valid.  kRegs: n <= REGS
+// NT, keys and tokens in registers and the table in shared memory; otherwise
+// every pass reads them again.
+template <int NT, int REGS, bool kRegs>
+__device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, EvShared<NT, REGS>& sh, int32_t* count) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
   const int n = s.n, shift = a.c.page_shift, mask = (1 << shift) - 1;
   auto place = [&](int j) {
     const int page = kRegs ? sh.pages[j >> shift] : s.table[j >> shift];
     return page_row(a.c, page, h) + (j & mask);
   };
-  uint32_t key[kEvRegs];
-  int tok[kEvRegs];
+  uint32_t key[REGS];
+  int tok[REGS];
   if constexpr (kRegs) {
 #pragma unroll
-    for (int u0 = 0; u0 < kEvRegs; u0 += kEvUnit) {
+    for (int u0 = 0; u0 < REGS; u0 += kEvUnit) {
       if (u0 * NT < n) {
         int at[kEvUnit];
         float v[kEvUnit];
@@ -110,7 +108,7 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
   auto each = [&](const auto& fn) {
     if constexpr (kRegs) {
 #pragma unroll
-      for (int u0 = 0; u0 < kEvRegs; u0 += kEvUnit) {
+      for (int u0 = 0; u0 < REGS; u0 += kEvUnit) {
         if (u0 * NT < n) {
 #pragma unroll
           for (int u = 0; u < kEvUnit; ++u) {
@@ -163,7 +161,7 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
       cn += tk >= first_new ? 1u : 0u;
       co += tk <= last_old ? 1u : 0u;
     });
-    const uint2 c = block_sum2<NT>(cn, co, sh);
+    const uint2 c = block_sum2<NT, REGS>(cn, co, sh);
     auto all = [](uint32_t, int) { return true; };
     if (c.x != (uint32_t)r) first_new = (int)select(r, age_top, all, [](uint32_t, int tk) { return (uint32_t)tk; });
     if (c.y != (uint32_t)o)
@@ -194,7 +192,7 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
     constexpr int NW = NT / kWave;
     uint32_t out = 0, in = 0;  // bit u: row u of this thread is listed
 #pragma unroll
-    for (int u0 = 0; u0 < kEvRegs; u0 += kEvUnit) {
+    for (int u0 = 0; u0 < REGS; u0 += kEvUnit) {
 #pragma unroll
       for (int u = u0; u < u0 + kEvUnit; ++u) {
         const int j = u * NT + tid;
@@ -215,7 +213,7 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
     }
     __syncthreads();
     if (w < 2) {  // NT >= 128: one wave a list
-      constexpr int per = kEvRegs * NW / kWave;
+      constexpr int per = REGS * NW / kWave;
       int v[per], sum = 0;
 #pragma unroll
       for (int i = 0; i < per; ++i) {
@@ -234,7 +232,7 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
     __syncthreads();
     const int moves = min(sh.total[0], sh.total[1]);  // equal where tokens are distinct
 #pragma unroll
-    for (int u = 0; u < kEvRegs; ++u) {
+    for (int u = 0; u < REGS; ++u) {
       if (u * NT < n) {
         const bool hole = (out >> u) & 1u, mover = (in >> u) & 1u;
         const unsigned long long below = (1ull << lane) - 1ull;
@@ -276,18 +274,18 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
   }
 }
 
-template <int NT>
+template <int NT, int REGS>
 __global__ __launch_bounds__(NT) void select_kernel(PagedEvictArgs a) {
-  __shared__ EvShared<NT> sh;
+  __shared__ EvShared<NT, REGS> sh;
   const int h = blockIdx.x % a.c.HK;
   const EvSeq s = ev_seq(a, blockIdx.x / a.c.HK);
   int32_t* const count = a.count + blockIdx.x;
-  bool bad = s.n < 0 || s.n > ((long long)a.c.max_pages << a.c.page_shift) || s.seen < s.n;
+  bool bad = s.n < 0 || s.n > a.max_kv || s.seen < s.n;
   const int pages = bad ? 0 : (int)(((long long)s.n + (1 << a.c.page_shift) - 1) >> a.c.page_shift);
   for (int i = threadIdx.x; i < pages; i += NT) {
     const int page = s.table[i];
     bad = bad || page < 0 || page >= a.c.num_pages;
-    if (i < kEvPages) sh.pages[i] = page;
+    if (i < NT * REGS / 16) sh.pages[i] = page;
   }
   bad = __syncthreads_or(bad);
   if (bad || s.k >= s.n) {
@@ -297,10 +295,10 @@ __global__ __launch_bounds__(NT) void select_kernel(PagedEvictArgs a) {
     }
     return;
   }
-  if (s.n <= kEvRegs * NT)
-    select_segment<NT, true>(a, s, h, sh, count);
+  if (s.n <= REGS * NT)
+    select_segment<NT, REGS, true>(a, s, h, sh, count);
   else
-    select_segment<NT, false>(a, s, h, sh, count);
+    select_segment<NT, REGS, false>(a, s, h, sh, count);
 }
 
 // blockIdx.x = segment * parts + part: a segment's moves go round its parts.
@@ -354,16 +352,19 @@ __global__ __launch_bounds__(256) void move_kernel(PagedEvictArgs a, int parts) 
 lethe_status launch_paged_evict(const PagedEvictArgs& a, hipStream_t s) {
   const long long segs = (long long)a.L * a.c.B * a.c.HK;
   if (segs * 1024 > 0xffffffffLL) return LETHE_ERR_UNSUPPORTED;  // threads of a launch stay below 2^32
-  const long long room = (long long)a.c.max_pages << a.c.page_shift;
-  // 256 threads hold 8192 rows, 1024 threads 32768.
-  if (room <= kEvRegs * 256)
-    hipLaunchKernelGGL(select_kernel<256>, dim3((unsigned)segs), dim3(256), 0, s, a);
+  // The fewest threads that hold the rows.
+  if (a.max_kv <= 16 * 256)
+    hipLaunchKernelGGL((select_kernel<256, 16>), dim3((unsigned)segs), dim3(256), 0, s, a);
+  else if (a.max_kv <= 16 * 512)
+    hipLaunchKernelGGL((select_kernel<512, 16>), dim3((unsigned)segs), dim3(512), 0, s, a);
+  else if (a.max_kv <= 24 * 1024)
+    hipLaunchKernelGGL((select_kernel<1024, 24>), dim3((unsigned)segs), dim3(1024), 0, s, a);
   else
-    hipLaunchKernelGGL(select_kernel<1024>, dim3((unsigned)segs), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((select_kernel<1024, 32>), dim3((unsigned)segs), dim3(1024), 0, s, a);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   // Enough blocks to fill the chip however few the segments are, but no more
   // than a segment's largest number of moves has use for.
-  const long long most = (room / 2 + 63) / 64;
+  const long long most = (a.max_kv / 2 + 63) / 64;
   const int parts = (int)std::max(1LL, std::min({most, 4096LL / segs, 1024LL}));
   const auto kernel = a.D == 128 ? move_kernel<128> : move_kernel<64>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(segs * parts)), dim3(256), 0, s, a, parts);

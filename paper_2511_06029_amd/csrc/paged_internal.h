@@ -67,7 +67,7 @@ struct PagedEvictArgs {
   PagedView c;           // layer 0: len, seen and table hold every layer
   int32_t L, D;
   const int32_t* budget; // [B][L]
-  int32_t recent, sink;
+  int32_t recent, sink, max_kv;
   int32_t* count;        // [L][B][HK] moves of a segment, or kEvict* codes
   int2* moves;           // (destination, source) pool rows: a segment's i-th at the place of its row i
 };

@@ -122,7 +122,7 @@ def load():
         lib.lethe_paged_attn_score.restype = ctypes.c_int
         lib.lethe_paged_attn_workspace_bytes.argtypes = [pp, i64, i32, i32]
         lib.lethe_paged_attn_workspace_bytes.restype = sz
-        lib.lethe_paged_evict.argtypes = [pp, vp, i32, i32, vp, sz, vp]
+        lib.lethe_paged_evict.argtypes = [pp, vp, i32, i32, i32, vp, sz, vp]
         lib.lethe_paged_evict.restype = ctypes.c_int
         lib.lethe_paged_evict_workspace_bytes.argtypes = [pp]
         lib.lethe_paged_evict_workspace_bytes.restype = sz
@@ -343,13 +343,14 @@ def paged_attn_score(cache, layer, q, q_start, q_len, max_q_len, max_kv_len, gam
     _check(fn, st)
 
 
-def paged_evict(cache, budget, recent, sink, ws, stream=None):
+def paged_evict(cache, budget, recent, sink, ws, max_kv_len=None, stream=None):
     """lethe_paged_evict: bring every segment to its budget (int32 [num_seqs][num_layers]); updates len.  ws from
-    cache.evict_workspace."""
+    cache.evict_workspace; max_kv_len: an upper bound of the lengths (default: the tables' room)."""
     fn = "lethe_paged_evict"
     if str(budget.dtype) != "torch.int32" or not budget.is_contiguous() or tuple(budget.shape) != (cache.B, cache.L):
         raise LetheError(fn, ERR_INVALID)
-    st = load().lethe_paged_evict(ctypes.byref(cache.c_struct()), _p(budget), int(recent), int(sink), _p(ws),
+    st = load().lethe_paged_evict(ctypes.byref(cache.c_struct()), _p(budget), int(recent), int(sink),
+                                  0x7fffffff if max_kv_len is None else int(max_kv_len), _p(ws),
                                   ws.numel() * ws.element_size(), _stream(stream))
     _check(fn, st)
 

@@ -38,8 +38,8 @@ def attn(c, layer=0, q=FAKE, start=FAKE, length=FAKE, rows=4, most=1, kv=100, ga
                                            out, ws, wsb, None)
 
 
-def evict(c, budget=FAKE, recent=1, sink=0, ws=FAKE, wsb=BIG):
-    return L.load().lethe_paged_evict(ctypes.byref(c), budget, recent, sink, ws, wsb, None)
+def evict(c, budget=FAKE, recent=1, sink=0, kv=100, ws=FAKE, wsb=BIG):
+    return L.load().lethe_paged_evict(ctypes.byref(c), budget, recent, sink, kv, ws, wsb, None)
 
 
 @pytest.mark.parametrize("field,value,want", [
@@ -101,7 +101,7 @@ def test_attention_arguments():
 
 def test_eviction_arguments():
     c = make()
-    for kw in (dict(budget=None), dict(recent=-1), dict(sink=-1), dict(ws=None), dict(ws=FAKE + 8)):
+    for kw in (dict(budget=None), dict(recent=-1), dict(sink=-1), dict(kv=-1), dict(ws=None), dict(ws=FAKE + 8)):
         assert evict(c, **kw) == L.ERR_INVALID, kw
     assert evict(make(pos=None)) == L.ERR_INVALID and evict(make(seen=None)) == L.ERR_INVALID
     need = L.load().lethe_paged_evict_workspace_bytes(ctypes.byref(c))
