@@ -12,8 +12,13 @@
 //     registers (up to 32 rows a thread), the thresholds found by radix
 //     selection, the two lists (evicted before the budget, kept beyond it)
 //     ranked by ballots and one scan, and written as pairs.
-//  2. move_kernel: the pairs' rows, 16 bytes a lane, spread over the chip; the
-//     new lengths.
+//     With many segments its block moves the rows too.
+//  2. move_kernel: the pairs' rows, 16 bytes a lane, spread over the chip, and
+//     the new lengths; or length_kernel, the lengths alone.
+// Bound by the moved rows' bytes: a steady round (2048 segments of 2500 rows, a
+// fifth going) moves 0.9 GB in 215 us, selection included; 512 segments of
+// 16384 rows to 30% move 1.9 GB in 400 us, 4.8 TB/s, a copy's rate, after 61 us
+// of selection.
 #include <algorithm>
 
 #include "device_common.h"
@@ -24,6 +29,7 @@ namespace lethe {
 
 namespace {
 
+constexpr unsigned kEvWhole = 1024;  // segments from which on their blocks move the rows too
 constexpr int kEvUnit = 8;    // rows whose loads leave together
 
 // One (layer, sequence) of an eviction.
@@ -274,48 +280,16 @@ __device__ void select_segment(const PagedEvictArgs& a, const EvSeq& s, int h, E
   }
 }
 
-template <int NT, int REGS>
-__global__ __launch_bounds__(NT) void select_kernel(PagedEvictArgs a) {
-  __shared__ EvShared<NT, REGS> sh;
-  const int h = blockIdx.x % a.c.HK;
-  const EvSeq s = ev_seq(a, blockIdx.x / a.c.HK);
-  int32_t* const count = a.count + blockIdx.x;
-  bool bad = s.n < 0 || s.n > a.max_kv || s.seen < s.n;
-  const int pages = bad ? 0 : (int)(((long long)s.n + (1 << a.c.page_shift) - 1) >> a.c.page_shift);
-  for (int i = threadIdx.x; i < pages; i += NT) {
-    const int page = s.table[i];
-    bad = bad || page < 0 || page >= a.c.num_pages;
-    if (i < NT * REGS / 16) sh.pages[i] = page;
-  }
-  bad = __syncthreads_or(bad);
-  if (bad || s.k >= s.n) {
-    if (threadIdx.x == 0) {
-      if (bad) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
-      *count = kEvictNone;
-    }
-    return;
-  }
-  if (s.n <= REGS * NT)
-    select_segment<NT, REGS, true>(a, s, h, sh, count);
-  else
-    select_segment<NT, REGS, false>(a, s, h, sh, count);
-}
-
-// blockIdx.x = segment * parts + part: a segment's moves go round its parts.
-template <int D>
-__global__ __launch_bounds__(256) void move_kernel(PagedEvictArgs a, int parts) {
+// Moves of a segment by a block of NT threads, one of `parts` that take turns.
+template <int D, int NT>
+__device__ inline void move_rows(const PagedEvictArgs& a, const int32_t* table, int h, int moves, int part, int parts) {
   constexpr int LPR = D / 8;        // lanes a row: 16 bytes each
-  constexpr int RPB = 256 / LPR;    // rows of a block at a time
+  constexpr int RPB = NT / LPR;     // rows of a block at a time
   constexpr int U = 4;              // times that, loads before the first store
-  const int seg = blockIdx.x / parts, part = blockIdx.x % parts;
-  const int moves = a.count[seg];
-  if (moves == kEvictNone) return;
-  const int h = seg % a.c.HK, lb = seg / a.c.HK;
-  const EvSeq s = ev_seq(a, lb);  // len: written below by one block of the sequence, not used here
+  typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
   const int sub = threadIdx.x / LPR, piece = threadIdx.x % LPR;
   for (long long i0 = (long long)part * RPB * U; i0 < moves; i0 += (long long)parts * RPB * U) {
-    typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
     int2 e[U];
     u32x4_t kr[U], vr[U];
     float sc[U];
@@ -323,7 +297,7 @@ __global__ __launch_bounds__(256) void move_kernel(PagedEvictArgs a, int parts) 
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = (int)min(i0 + u * RPB + sub, (long long)moves - 1);
-      e[u] = a.moves[page_row(a.c, s.table[i >> shift], h) + (i & mask)];
+      e[u] = a.moves[page_row(a.c, table[i >> shift], h) + (i & mask)];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -344,8 +318,85 @@ __global__ __launch_bounds__(256) void move_kernel(PagedEvictArgs a, int parts) 
       }
     }
   }
+}
+
+// One block a segment.  D > 0: it moves the rows too (len is left to
+// length_kernel: another head's block may still have to read it).
+template <int NT, int REGS, int D>
+__global__ __launch_bounds__(NT) void select_kernel(PagedEvictArgs a) {
+  __shared__ EvShared<NT, REGS> sh;
+  __shared__ int moves;
+  const int h = blockIdx.x % a.c.HK;
+  const EvSeq s = ev_seq(a, blockIdx.x / a.c.HK);
+  int32_t* const count = a.count + blockIdx.x;
+  bool bad = s.n < 0 || s.n > a.max_kv || s.seen < s.n;
+  const int pages = bad ? 0 : (int)(((long long)s.n + (1 << a.c.page_shift) - 1) >> a.c.page_shift);
+  for (int i = threadIdx.x; i < pages; i += NT) {
+    const int page = s.table[i];
+    bad = bad || page < 0 || page >= a.c.num_pages;
+    if (i < NT * REGS / 16) sh.pages[i] = page;
+  }
+  bad = __syncthreads_or(bad);
+  if (bad || s.k >= s.n) {
+    if (threadIdx.x == 0) {
+      if (bad) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
+      *count = kEvictNone;
+    }
+    return;
+  }
+  if (s.n <= REGS * NT)
+    select_segment<NT, REGS, true>(a, s, h, sh, &moves);
+  else
+    select_segment<NT, REGS, false>(a, s, h, sh, &moves);
+  if (threadIdx.x == 0) *count = moves;
+  if constexpr (D > 0) {
+    __threadfence_block();
+    __syncthreads();
+    move_rows<D, NT>(a, s.table, h, moves, 0, 1);
+  }
+}
+
+// blockIdx.x = segment * parts + part.
+template <int D>
+__global__ __launch_bounds__(256) void move_kernel(PagedEvictArgs a, int parts) {
+  const int seg = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int moves = a.count[seg];
+  if (moves == kEvictNone) return;
+  const int h = seg % a.c.HK, lb = seg / a.c.HK;
+  const EvSeq s = ev_seq(a, lb);  // len: written below by one block of the sequence, not used here
+  move_rows<D, 256>(a, s.table, h, moves, part, parts);
   if (h == 0 && part == 0 && threadIdx.x == 0) a.c.len[lb] = s.k;
 }
+
+__global__ __launch_bounds__(256) void length_kernel(PagedEvictArgs a) {
+  const int lb = blockIdx.x * 256 + threadIdx.x;
+  if (lb < a.L * a.c.B && a.count[(long long)lb * a.c.HK] != kEvictNone) a.c.len[lb] = ev_seq(a, lb).k;
+}
+
+template <int NT, int REGS>
+lethe_status launch(const PagedEvictArgs& a, unsigned segs, hipStream_t s) {
+  // Blocks that move what they have ranked overlap the two, if they are many
+  // (a fifth of 2500 rows going: 2048 segments 246 us against 261 in two
+  // launches, 1024 129 against 134, 512 74 both, 128 34 against 28).
+  const bool whole = segs >= kEvWhole;
+  if (whole) {
+    const auto kernel = a.D == 128 ? select_kernel<NT, REGS, 128> : select_kernel<NT, REGS, 64>;
+    hipLaunchKernelGGL(kernel, dim3(segs), dim3(NT), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
+    hipLaunchKernelGGL(length_kernel, dim3((a.L * a.c.B + 255) / 256), dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+  }
+  hipLaunchKernelGGL((select_kernel<NT, REGS, 0>), dim3(segs), dim3(NT), 0, s, a);
+  if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
+  // Enough blocks to fill the chip however few the segments are, but no more
+  // than a segment's largest number of moves has use for.
+  const long long most = (a.max_kv / 2 + 63) / 64;
+  const int parts = (int)std::max(1LL, std::min({most, 4096LL / segs, 1024LL}));
+  const auto kernel = a.D == 128 ? move_kernel<128> : move_kernel<64>;
+  hipLaunchKernelGGL(kernel, dim3(segs * parts), dim3(256), 0, s, a, parts);
+  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+}
+
 
 }  // namespace
 
@@ -353,22 +404,10 @@ lethe_status launch_paged_evict(const PagedEvictArgs& a, hipStream_t s) {
   const long long segs = (long long)a.L * a.c.B * a.c.HK;
   if (segs * 1024 > 0xffffffffLL) return LETHE_ERR_UNSUPPORTED;  // threads of a launch stay below 2^32
   // The fewest threads that hold the rows.
-  if (a.max_kv <= 16 * 256)
-    hipLaunchKernelGGL((select_kernel<256, 16>), dim3((unsigned)segs), dim3(256), 0, s, a);
-  else if (a.max_kv <= 16 * 512)
-    hipLaunchKernelGGL((select_kernel<512, 16>), dim3((unsigned)segs), dim3(512), 0, s, a);
-  else if (a.max_kv <= 24 * 1024)
-    hipLaunchKernelGGL((select_kernel<1024, 24>), dim3((unsigned)segs), dim3(1024), 0, s, a);
-  else
-    hipLaunchKernelGGL((select_kernel<1024, 32>), dim3((unsigned)segs), dim3(1024), 0, s, a);
-  if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
-  // Enough blocks to fill the chip however few the segments are, but no more
-  // than a segment's largest number of moves has use for.
-  const long long most = (a.max_kv / 2 + 63) / 64;
-  const int parts = (int)std::max(1LL, std::min({most, 4096LL / segs, 1024LL}));
-  const auto kernel = a.D == 128 ? move_kernel<128> : move_kernel<64>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(segs * parts)), dim3(256), 0, s, a, parts);
-  return hipGetLastError() == hipSuccess ? LETHE_OK : LETHE_ERR_HIP;
+  if (a.max_kv <= 16 * 256) return launch<256, 16>(a, (unsigned)segs, s);
+  if (a.max_kv <= 16 * 512) return launch<512, 16>(a, (unsigned)segs, s);
+  if (a.max_kv <= 24 * 1024) return launch<1024, 24>(a, (unsigned)segs, s);
+  return launch<1024, 32>(a, (unsigned)segs, s);
 }
 
 }  // namespace lethe

@@ -296,11 +296,34 @@ def decode_attn_score_compact(cache, layer, q, k_new, v_new, gamma, softmax_scal
 
 def _row_stride(fn, t, heads, dim, dtype):
     """Elements between the rows of a [rows][heads][dim] tensor whose heads lie side by side."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype:
+    rows, h, d = t.shape if t.dim() == 3 else (0, -1, -1)
+    if h != heads or d != dim or t.dtype != dtype:
         raise LetheError(fn, ERR_INVALID)
-    if t.shape[0] and ((dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim)):
+    row, head, elem = t.stride()
+    if rows and (elem != 1 or (heads > 1 and head != dim)):
         raise LetheError(fn, ERR_INVALID)
-    return t.stride(0) if t.shape[0] > 1 else heads * dim
+    return row if rows > 1 else heads * dim
+
+
+def _check_batch(fn, cache, q_start, q_len):
+    if (q_start.dtype != cache.torch.int64 or q_len.dtype != cache.torch.int32 or q_start.numel() != cache.B or
+            q_len.numel() != cache.B or not q_start.is_contiguous() or not q_len.is_contiguous()):
+        raise LetheError(fn, ERR_INVALID)
+
+
+def _paged_call(fn, cache, stream, *args):
+    """A call of the library on the cache's device and, by default, its current stream."""
+    cuda = cache.torch.cuda
+    if cuda.current_device() != cache.device.index:
+        with cuda.device(cache.device):
+            return _paged_call(fn, cache, stream, *args)
+    if stream is None:
+        stream = cuda.current_stream().cuda_stream
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    st = getattr(load(), fn)(cache.ref, *args, stream)
+    if st != OK:
+        raise LetheError(fn, st)
 
 
 def paged_append(cache, layer, q, k_new, v_new, q_start, q_len, max_q_len, rotary, q_out, stream=None):
@@ -309,21 +332,22 @@ def paged_append(cache, layer, q, k_new, v_new, q_start, q_len, max_q_len, rotar
     rotary None rotates nothing."""
     fn = "lethe_paged_append"
     rows = k_new.shape[0]
-    kd, vd = (_row_stride(fn, t, cache.HK, cache.D, cache.tdtype) for t in (k_new, v_new))
-    qd = 0 if q is None else _row_stride(fn, q, cache.HQ, cache.D, cache.tdtype)
+    kd = _row_stride(fn, k_new, cache.HK, cache.D, cache.tdtype)
+    vd = _row_stride(fn, v_new, cache.HK, cache.D, cache.tdtype)
+    qd, qp, op = 0, None, None
+    if q is not None:
+        qd, qp = _row_stride(fn, q, cache.HQ, cache.D, cache.tdtype), q.data_ptr()
     if v_new.shape[0] != rows or (q is not None and q.shape[0] != rows):
         raise LetheError(fn, ERR_INVALID)
-    if q_out is not None and (q_out.dtype != cache.tdtype or not q_out.is_contiguous() or
-                              tuple(q_out.shape) != (rows, cache.HQ, cache.D)):
-        raise LetheError(fn, ERR_INVALID)
+    if q_out is not None:
+        if q_out.dtype != cache.tdtype or not q_out.is_contiguous() or q_out.shape != (rows, cache.HQ, cache.D):
+            raise LetheError(fn, ERR_INVALID)
+        op = q_out.data_ptr()
     if rotary is not None and rotary.rows != rows:
         raise LetheError(fn, ERR_INVALID)
     _check_batch(fn, cache, q_start, q_len)
-    st = load().lethe_paged_append(ctypes.byref(cache.c_struct()), int(layer), _p(q), qd, _p(k_new), kd, _p(v_new), vd,
-                                   _p(q_start), _p(q_len), int(rows), int(max_q_len),
-                                   None if rotary is None else ctypes.byref(rotary.c_struct()), _p(q_out),
-                                   _stream(stream))
-    _check(fn, st)
+    _paged_call(fn, cache, stream, layer, qp, qd, k_new.data_ptr(), kd, v_new.data_ptr(), vd, q_start.data_ptr(),
+                q_len.data_ptr(), rows, max_q_len, None if rotary is None else rotary.ref, op)
 
 
 def paged_attn_score(cache, layer, q, q_start, q_len, max_q_len, max_kv_len, gamma, softmax_scale, softcap, out, ws,
@@ -332,33 +356,23 @@ def paged_attn_score(cache, layer, q, q_start, q_len, max_q_len, max_kv_len, gam
     the score update where gamma > 0; scores capped by softcap * tanh(x / softcap) where softcap > 0.  q and out:
     [rows][H_Q][D] in the cache's type, contiguous; ws from cache.attn_workspace."""
     fn = "lethe_paged_attn_score"
+    rows = q.shape[0]
     for t in (q, out):
-        if t.dtype != cache.tdtype or not t.is_contiguous() or tuple(t.shape) != (q.shape[0], cache.HQ, cache.D):
+        if t.dtype != cache.tdtype or not t.is_contiguous() or t.shape != (rows, cache.HQ, cache.D):
             raise LetheError(fn, ERR_INVALID)
     _check_batch(fn, cache, q_start, q_len)
-    st = load().lethe_paged_attn_score(ctypes.byref(cache.c_struct()), int(layer), _p(q), _p(q_start), _p(q_len),
-                                       int(q.shape[0]), int(max_q_len), int(max_kv_len), float(gamma),
-                                       float(softmax_scale), float(softcap), _p(out), _p(ws),
-                                       ws.numel() * ws.element_size(), _stream(stream))
-    _check(fn, st)
+    _paged_call(fn, cache, stream, layer, q.data_ptr(), q_start.data_ptr(), q_len.data_ptr(), rows, max_q_len,
+                max_kv_len, gamma, softmax_scale, softcap, out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def paged_evict(cache, budget, recent, sink, ws, max_kv_len=None, stream=None):
     """lethe_paged_evict: bring every segment to its budget (int32 [num_seqs][num_layers]); updates len.  ws from
     cache.evict_workspace; max_kv_len: an upper bound of the lengths (default: the tables' room)."""
     fn = "lethe_paged_evict"
-    if str(budget.dtype) != "torch.int32" or not budget.is_contiguous() or tuple(budget.shape) != (cache.B, cache.L):
+    if budget.dtype != cache.torch.int32 or not budget.is_contiguous() or budget.shape != (cache.B, cache.L):
         raise LetheError(fn, ERR_INVALID)
-    st = load().lethe_paged_evict(ctypes.byref(cache.c_struct()), _p(budget), int(recent), int(sink),
-                                  0x7fffffff if max_kv_len is None else int(max_kv_len), _p(ws),
-                                  ws.numel() * ws.element_size(), _stream(stream))
-    _check(fn, st)
-
-
-def _check_batch(fn, cache, q_start, q_len):
-    for t, name in ((q_start, "torch.int64"), (q_len, "torch.int32")):
-        if str(t.dtype) != name or not t.is_contiguous() or t.numel() != cache.B:
-            raise LetheError(fn, ERR_INVALID)
+    _paged_call(fn, cache, stream, budget.data_ptr(), recent, sink, 0x7fffffff if max_kv_len is None else max_kv_len,
+                ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 class Rotary:
@@ -378,8 +392,7 @@ class Rotary:
         self._c = CRotary(inv_freq.data_ptr(), axis_pos.data_ptr(), 2 * inv_freq.numel(), len(sections),
                           (ctypes.c_int32 * MAX_AXES)(*full), int(bool(adjacent)))
 
-    def c_struct(self):
-        return self._c
+        self.ref = ctypes.byref(self._c)
 
 
 class LethePagedCache:
@@ -410,6 +423,7 @@ class LethePagedCache:
         self._c = CPagedCache(k.data_ptr(), v.data_ptr(), score.data_ptr(), pos.data_ptr(), len_.data_ptr(),
                               seen.data_ptr(), page_table.data_ptr(), self.num_pages, self.page_size, self.max_pages,
                               self.L, self.B, self.HQ, self.HK, self.D, codes[k.dtype], self.dev_status.data_ptr())
+        self.device, self.ref = k.device, ctypes.byref(self._c)
         if self.evict_workspace_bytes() == 0:
             raise LetheError("LethePagedCache", ERR_UNSUPPORTED)
 
@@ -426,22 +440,19 @@ class LethePagedCache:
                    make((num_layers, num_seqs), torch.int32),
                    torch.full((num_layers, num_seqs, max_pages), -1, dtype=torch.int32, device=device), num_q_heads)
 
-    def c_struct(self):
-        return self._c
-
     def evict_workspace_bytes(self):
-        return int(load().lethe_paged_evict_workspace_bytes(ctypes.byref(self._c)))
+        return int(load().lethe_paged_evict_workspace_bytes(self.ref))
 
     def evict_workspace(self):
-        return self.torch.empty(self.evict_workspace_bytes(), dtype=self.torch.uint8, device=self.k.device)
+        return self.torch.empty(self.evict_workspace_bytes(), dtype=self.torch.uint8, device=self.device)
 
     def attn_workspace(self, q_rows, max_q_len, max_kv_len):
         """Workspace of paged_attn_score for calls within these bounds."""
-        n = int(load().lethe_paged_attn_workspace_bytes(ctypes.byref(self._c), int(q_rows), int(max_q_len),
+        n = int(load().lethe_paged_attn_workspace_bytes(self.ref, int(q_rows), int(max_q_len),
                                                         int(max_kv_len)))
         if n == 0:
             raise LetheError("lethe_paged_attn_workspace_bytes", ERR_UNSUPPORTED)
-        return self.torch.empty(n, dtype=self.torch.uint8, device=self.k.device)
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.device)
 
 
 class LetheCache:
