@@ -5,15 +5,15 @@
 // columns of one product: column c is query c / G, head c % G, so a group's
 // keys and values are read once for all of them whatever G and q_len are.
 //
-// One query a sequence (max_q_len <= 1), bound by the rows' bytes:
+// Up to 16 columns (one query, or a few), bound by the rows' bytes:
 //  1. decode_kernel: the rows of every (sequence, KV head) cut into chunks of
 //     like length, one block each; a wavefront takes 32 rows at a time on
-//     16x16x32 products, G columns of 16 in use.  Writes a chunk's (max, sum,
-//     output) and, for the scores, the rows' logits.
+//     16x16x32 products.  Writes a chunk's (max, sum, output) and, for the
+//     scores, the rows' logits.
 //  2. finish_kernel: joins a segment's chunks and turns the logits into
 //     weights once the segment's max and sum are known.
 //
-// Longer queries, bound by the products:
+// More columns, bound by the products (sequences with few decode beside them):
 //  1. plan_kernel (one block): cuts every (sequence, 128 columns) into key
 //     ranges of like work and orders them, longest first.
 //  2. tile_kernel: flash attention forward of 128 columns over a key range,
@@ -120,8 +120,12 @@ __device__ inline void barrier_only() {
 }
 
 // ---------------------------------------------------------------------------
-// One query a sequence
+// Few columns
 // ---------------------------------------------------------------------------
+constexpr int kFewCols = 16;
+__device__ inline bool few_cols(const PagedAttnArgs& a, int ql) { return ql > 0 && ql <= kFewCols / a.G; }
+// Columns that a call's partials and logits have room for.
+__host__ __device__ inline int room_cols(int max_q, int G) { return max_q > kFewCols / G ? kFewCols / G * G : max_q * G; }
 constexpr int kDecStep = 32;        // rows a wavefront takes at a time
 constexpr int kDecMaxChunks = 64;   // of a segment
 constexpr int kDecChunkSteps = 14;  // steps of a chunk, where there are enough
@@ -144,13 +148,13 @@ __host__ __device__ inline int dec_chunks(int steps, int per) {
   const int nch = (steps + per - 1) / per;
   return nch < kDecMaxChunks ? nch : kDecMaxChunks;
 }
-// Floats of a chunk's partial: (max, sum) and output of every head.
-__host__ __device__ inline int dec_part(int G, int D) { return (G * (D + 2) + 31) / 32 * 32; }
+// Floats of a chunk's partial: (max, sum) and output of every column.
+__host__ __device__ inline int dec_part(int cols, int D) { return (cols * (D + 2) + 31) / 32 * 32; }
 
 struct DecChunk {
-  int b, h, c, nch, n;
+  int b, h, c, nch, n, ql;
   int first;               // block index of the segment's chunk 0
-  long long row0;          // rows of the segments before it, rounded up to steps: its logits start at row0 G
+  long long row0;          // rows of the segments before it, rounded up to steps: its logits start at row0 room_cols
   long long q0;
 };
 
@@ -160,15 +164,16 @@ struct DecChunk {
 template <int R>
 __device__ inline bool dec_chunk(const PagedAttnArgs& a, int idx, int seg, DecChunk& ck) {
   const int lane = threadIdx.x & (kWave - 1);
-  int steps[R], rows[R];
+  int steps[R], rows[R], queries[R];
   int total = 0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int b = kWave * r + lane;
-    steps[r] = rows[r] = 0;
+    steps[r] = rows[r] = queries[r] = 0;
     if (b < a.c.B) {
       const AttnSeq s = attn_seq(a, b);
-      if (s.ok && s.ql == 1) {
+      if (s.ok && few_cols(a, s.ql)) {
+        queries[r] = s.ql;
         rows[r] = s.n;
         steps[r] = (s.n + kDecStep - 1) / kDecStep;
       } else if (!s.ok && blockIdx.x == 0 && threadIdx.x < kWave) {
@@ -193,6 +198,7 @@ __device__ inline bool dec_chunk(const PagedAttnArgs& a, int idx, int seg, DecCh
       ck.b = kWave * r + l;
       ck.nch = __builtin_amdgcn_readlane(nch, l);
       ck.n = __builtin_amdgcn_readlane(rows[r], l);
+      ck.ql = __builtin_amdgcn_readlane(queries[r], l);
       const int st = __builtin_amdgcn_readlane(steps[r], l);
       if (ck.nch == 0) return false;
       const int at = blocks0 + __builtin_amdgcn_readlane(incl, l) - ck.nch * a.c.HK;
@@ -234,13 +240,12 @@ __device__ inline bool dec_room(const DecWs& ws, const DecChunk& ck) {
   return ck.row0 + (ck.n + kDecStep - 1) / kDecStep * kDecStep <= ws.logit_rows;
 }
 
-constexpr int kMaxG = 8;
-
 // One chunk by a block of kThreads; its partial goes to slot `slot`.  tile(w):
-// LDS of wave w, DecCfg::VTILE bytes.
-template <typename T, int D, bool kCap, class Tile>
+// LDS of wave w, DecCfg::VTILE bytes.  kOne: sequences have one query, which
+// attends every row (the masks of several cost registers that the loop spills).
+template <typename T, int D, bool kCap, bool kOne, class Tile>
 __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, const DecChunk& ck, long long slot,
-                                    const Tile& tile, float2 (&wave_ml)[kNumWaves][kMaxG]) {
+                                    const Tile& tile, float2 (&wave_ml)[kNumWaves][kFewCols]) {
   using Cfg = DecCfg<D>;
   using M = Mma<T>;
   constexpr int KK = Cfg::KK, NT = Cfg::NT, ROWB = Cfg::ROWB, LPR = Cfg::LPR, VLOADS = Cfg::VLOADS;
@@ -248,20 +253,22 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
   const int lane = tid & (kWave - 1);
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int g4 = lane >> 4, s = lane & 15;
-  const int G = a.G;
-  const int n = ck.n;
+  const int n = ck.n, cols = kOne ? a.G : ck.ql * a.G;
+  const int full = n - ck.ql;                 // rows up to it are attended by every column
+  const int query = kOne ? 0 : query_of(a, s);
+  const int lim = full + query;               // last row of column s
   const int steps = (n + kDecStep - 1) / kDecStep;
   const int first = (int)((long long)steps * ck.c / ck.nch), end = (int)((long long)steps * (ck.c + 1) / ck.nch);
   lds_char* const vb = (lds_char*)tile(w);
 
   // Queries as the B operand of S^T = K Q^T: lane (g4, s) holds
-  // Q[head s][dims 32 kk + 8 g4 ..], heads past G zero.
+  // Q[column s][dims 32 kk + 8 g4 ..], columns past the last zero.
   typename M::x8 qb[KK];
   {
-    const char* q = (const char*)a.q + (ck.q0 * a.c.HQ + (long long)ck.h * G) * ROWB;
+    const char* q = (const char*)a.q + ((ck.q0 + query) * a.c.HQ + ck.h * a.G + s - query * a.G) * (long long)ROWB;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
-      qb[kk] = s < G ? *reinterpret_cast<const typename M::x8*>(q + s * ROWB + 64 * kk + 16 * g4) : mma_zero<T>();
+      qb[kk] = s < cols ? *reinterpret_cast<const typename M::x8*>(q + 64 * kk + 16 * g4) : mma_zero<T>();
   }
 
   // Granules of this wave's next 32 steps, two a step: lane 2 i + g holds
@@ -323,9 +330,10 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) o[nt] = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   const Logit<kCap> lg(a);
-  // Logits, [step][head][row of the step]: a step's lie side by side.
-  float* const logit =
-      a.gamma > 0.0f && dec_room(ws, ck) && s < G ? ws.logit + ck.row0 * G + s * kDecStep + 4 * g4 : nullptr;
+  // Logits, [step][column][row of the step]: a step's lie side by side.
+  float* const logit = a.gamma > 0.0f && dec_room(ws, ck) && s < cols
+                           ? ws.logit + ck.row0 * room_cols(a.max_q, a.G) + s * kDecStep + 4 * g4
+                           : nullptr;
 
   int step = first + w, i = 0;
   if (step < end) {
@@ -339,7 +347,7 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
     const int next = step + kNumWaves;
     const bool b0 = bad && g0 < 0, b1 = bad && g1 < 0;  // of this step
     // Rows of the step that take no part (wave-uniform).
-    const uint32_t dead = (n - base < kDecStep ? ~0u << (n - base) : 0u) | (b0 ? 0xffffu : 0u) | (b1 ? 0xffff0000u : 0u);
+    uint32_t dead = (n - base < kDecStep ? ~0u << (n - base) : 0u) | (b0 ? 0xffffu : 0u) | (b1 ? 0xffff0000u : 0u);
     mma_f32x4_t x[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -355,17 +363,19 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
       granules(i);
       load_k(next * kDecStep);
     }
-    // Logits of rows base + 16 t + 4 g4 + r for head s.
+    // Logits of rows base + 16 t + 4 g4 + r for column s.
+    const bool edge = !kOne && base + kDecStep - 1 > full;  // some columns do not attend some rows
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         x[t][r] = lg.logit(lg.value(x[t][r]));
         if (dead && ((dead >> (16 * t + 4 * g4 + r)) & 1u)) x[t][r] = -INFINITY;
+        if (edge && base + 16 * t + 4 * g4 + r > lim) x[t][r] = -INFINITY;
       }
     if (logit) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) *reinterpret_cast<mma_f32x4_t*>(logit + (long long)base * G + 16 * t) = x[t];
+      for (int t = 0; t < 2; ++t) *reinterpret_cast<mma_f32x4_t*>(logit + (long long)base * cols + 16 * t) = x[t];
     }
     float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                      fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
@@ -394,6 +404,23 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
       const typename M::x4 a0 = M::read_tr(vb + Cfg::vaddr(rsub, col)), a1 = M::read_tr(vb + Cfg::vaddr(rsub + 16, col));
       return __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
     };
+    uint32_t apart = 0;
+    if (edge && full + 1 < n) {
+      // Rows that only some columns attend stay out of the products where they
+      // hold an infinity or NaN, and are added one by one.
+      const int r0 = max(full + 1 - base, 0), r1 = min(n - base, kDecStep);
+      for (int x0 = r0 * LPR; x0 < r1 * LPR; x0 += kWave) {
+        const int i = min(x0 + lane, r1 * LPR - 1);
+        const uint4 v = *reinterpret_cast<const uint4*>(tile(w) + Cfg::vaddr(i / LPR, 16 * (i % LPR)));
+        unsigned long long hit = __ballot(M::odd(v));
+        while (hit) {  // rare
+          apart |= 1u << (min(x0 + (int)__builtin_ctzll(hit), r1 * LPR - 1) / LPR);
+          hit &= hit - 1;
+        }
+      }
+      apart &= ~dead;
+      dead |= apart;
+    }
     if (!dead) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) o[nt] = M::mma16(operand(nt), p, o[nt]);
@@ -406,6 +433,25 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
           if ((dead >> (16 * (j >> 2) + 4 * g4 + (j & 3))) & 1u) av[j] = (T)0.0f;
         o[nt] = M::mma16(av, p, o[nt]);
       }
+      if (apart) {
+        float pw[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pw[j] = (float)p[j];
+#pragma unroll 1
+        while (apart) {
+          const int r = (int)__builtin_ctz(apart);
+          apart &= apart - 1;
+          const float pr = __shfl(pw[4 * (r >> 4) + (r & 3)], 16 * ((r >> 2) & 3) + s);
+          if (base + r <= lim) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                o[nt][x] = fmaf(pr, (float)*reinterpret_cast<const T*>(tile(w) + Cfg::vaddr(r, 2 * (16 * nt + 4 * g4 + x))),
+                                o[nt][x]);
+          }
+        }
+      }
     }
     if (next < end) {
       // The tile's reads are done (their results are in the products above).
@@ -415,87 +461,86 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
     step = next;
   }
 
-  // Lane groups hold different rows of the same heads.
+  // Lane groups hold different rows of the same columns.
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   // The waves' parts of the chunk, joined in LDS: outputs transposed through
-  // this wave's own V tile, [head][dim].
-  if (g4 == 0 && s < G) wave_ml[w][s] = make_float2(m, l);
-  static_assert(Cfg::VTILE >= kMaxG * D * 4, "a wave's outputs fit its V tile");
+  // this wave's own V tile, [column][dim].
+  if (g4 == 0 && s < cols) wave_ml[w][s] = make_float2(m, l);
+  static_assert(Cfg::VTILE >= kFewCols * D * 4, "a wave's outputs fit its V tile");
   wait_vmem();
   __builtin_amdgcn_s_waitcnt(0xc07f);
-  if (s < G) {
+  if (s < cols) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
       *(__attribute__((address_space(3))) mma_f32x4_t*)(vb + (s * D + 16 * nt + 4 * g4) * 4) = o[nt];
   }
   __syncthreads();
-  float* const part = ws.part + slot * dec_part(G, D);
-  for (int x = tid; x < G * D; x += kThreads) {
-    const int g = x / D;
-    float mm = wave_ml[0][g].x;
+  float* const part = ws.part + slot * dec_part(room_cols(a.max_q, a.G), D);
+  for (int x = tid; x < cols * D; x += kThreads) {
+    const int c = x / D;
+    float mm = wave_ml[0][c].x;
 #pragma unroll
-    for (int v = 1; v < kNumWaves; ++v) mm = fmaxf(mm, wave_ml[v][g].x);
+    for (int v = 1; v < kNumWaves; ++v) mm = fmaxf(mm, wave_ml[v][c].x);
     float sum = 0.0f, lsum = 0.0f;
 #pragma unroll
     for (int v = 0; v < kNumWaves; ++v) {
-      const float f = hw_exp2(wave_ml[v][g].x - mm);
+      const float f = hw_exp2(wave_ml[v][c].x - mm);
       sum = fmaf(f, *reinterpret_cast<const float*>(tile(v) + x * 4), sum);
-      lsum = fmaf(f, wave_ml[v][g].y, lsum);
+      lsum = fmaf(f, wave_ml[v][c].y, lsum);
     }
-    part[2 * G + x] = sum;
-    if (x % D == 0) *reinterpret_cast<float2*>(part + 2 * g) = make_float2(mm, lsum);
+    part[2 * cols + x] = sum;
+    if (x % D == 0) *reinterpret_cast<float2*>(part + 2 * c) = make_float2(mm, lsum);
   }
 }
 
-template <typename T, int D, bool kCap, int R>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3))) void decode_kernel(PagedAttnArgs a, DecWs ws) {
+template <typename T, int D, bool kCap, int R, bool kOne>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kOne ? 3 : 2))) void decode_kernel(PagedAttnArgs a, DecWs ws) {
   __shared__ __attribute__((aligned(16))) char vtiles[kNumWaves * DecCfg<D>::VTILE];
-  __shared__ float2 wave_ml[kNumWaves][kMaxG];
+  __shared__ float2 wave_ml[kNumWaves][kFewCols];
   DecChunk ck;
   if (!dec_chunk<R>(a, blockIdx.x, -1, ck)) return;
-  decode_chunk<T, D, kCap>(a, ws, ck, blockIdx.x, [&](int w) { return vtiles + w * DecCfg<D>::VTILE; }, wave_ml);
+  decode_chunk<T, D, kCap, kOne>(a, ws, ck, blockIdx.x, [&](int w) { return vtiles + w * DecCfg<D>::VTILE; }, wave_ml);
 }
 
-// What is left of a segment with one query: y = 0: its output, y > 0: the
+// What is left of a segment with few columns: y = 0: its output, y > 0: the
 // scores of its rows from (y - 1) span on.  Every block joins the chunks'
 // statistics.
 template <typename T, int D, int R>
 __device__ inline void finish_segment(const PagedAttnArgs& a, const DecWs& ws, int span, int seg, long long y) {
-  __shared__ float factor[kMaxG][kDecMaxChunks];  // what a chunk's output counts
-  __shared__ float2 stat[kMaxG];                  // max, 1 / sum
+  __shared__ float factor[kFewCols][kDecMaxChunks];  // what a chunk's output counts
+  __shared__ float2 stat[kFewCols];                  // max, 1 / sum
   const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
   DecChunk ck;
   if (!dec_chunk<R>(a, -1, seg, ck)) return;
   const long long r0 = (y - 1) * span;
   if (y > 0 && r0 >= ck.n) return;
-  const int G = a.G, pstride = dec_part(G, D);
+  const int cols = ck.ql * a.G, room = room_cols(a.max_q, a.G), pstride = dec_part(room, D);
   const float* const part = ws.part + (long long)ck.first * pstride;
-  for (int g = w; g < G; g += kNumWaves) {
-    const float2 ml = lane < ck.nch ? *reinterpret_cast<const float2*>(part + (long long)lane * pstride + 2 * g)
+  for (int c = w; c < cols; c += kNumWaves) {
+    const float2 ml = lane < ck.nch ? *reinterpret_cast<const float2*>(part + (long long)lane * pstride + 2 * c)
                                     : make_float2(kNegBig, 0.0f);
     const float mm = wave_max(ml.x);
     const float f = hw_exp2(ml.x - mm);
     const float sum = wave_sum(f * ml.y);
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // no row at all: 0
-    factor[g][lane] = f * inv;
-    if (lane == 0) stat[g] = make_float2(mm, inv);
+    factor[c][lane] = f * inv;
+    if (lane == 0) stat[c] = make_float2(mm, inv);
   }
   __syncthreads();
   if (y == 0) {
-    T* const out = (T*)a.out + (ck.q0 * a.c.HQ + (long long)ck.h * G) * D;
-    for (int x = tid; x < G * D; x += kThreads) {
-      const int g = x / D;
-      const float* const po = part + 2 * G + x;
+    for (int x = tid; x < cols * D; x += kThreads) {
+      const int c = x / D, query = query_of(a, c);
+      const float* const po = part + 2 * cols + x;
       float sum = 0.0f;
-      for (int c0 = 0; c0 < ck.nch; c0 += 8) {
+      for (int i0 = 0; i0 < ck.nch; i0 += 8) {
         float v[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = po[(long long)min(c0 + c, ck.nch - 1) * pstride];
+        for (int i = 0; i < 8; ++i) v[i] = po[(long long)min(i0 + i, ck.nch - 1) * pstride];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) sum = fmaf(c0 + c < ck.nch ? factor[g][c0 + c] : 0.0f, v[c], sum);
+        for (int i = 0; i < 8; ++i) sum = fmaf(i0 + i < ck.nch ? factor[c][i0 + i] : 0.0f, v[i], sum);
       }
-      out[x] = (T)sum;
+      ((T*)a.out)[((ck.q0 + query) * a.c.HQ + ck.h * a.G + c - query * a.G) * D + x % D] = (T)sum;
     }
     return;
   }
@@ -503,41 +548,38 @@ __device__ inline void finish_segment(const PagedAttnArgs& a, const DecWs& ws, i
     if (tid == 0) atomicOr(a.c.dev_status, LETHE_DEV_BAD_LAYOUT);
     return;
   }
-  const float* const logit = ws.logit + ck.row0 * G;
+  const float* const logit = ws.logit + ck.row0 * room;
   const int mask = (1 << a.c.page_shift) - 1;
   const int end = (int)min(r0 + span, (long long)ck.n);
   // Four rows a thread: their scores lie side by side (a page holds whole
   // granules of 16).
   for (int r = (int)r0 + 4 * tid; r < end; r += kFinUnit) {
     const int page = a.c.table[(long long)ck.b * a.c.max_pages + (r >> a.c.page_shift)];
-    mma_f32x4_t x[kMaxG];
+    const float* const xr = logit + (long long)(r / kDecStep) * cols * kDecStep + r % kDecStep;
+    mma_f32x4_t sum = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c0 = 0; c0 < cols; c0 += 8) {
+      mma_f32x4_t x[8];
 #pragma unroll
-    for (int g = 0; g < kMaxG; ++g)
-      if (g < G) x[g] = *reinterpret_cast<const mma_f32x4_t*>(logit + (long long)(r / kDecStep * G + g) * kDecStep + r % kDecStep);
+      for (int c = 0; c < 8; ++c)
+        if (c0 + c < cols) x[c] = *reinterpret_cast<const mma_f32x4_t*>(xr + (c0 + c) * kDecStep);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c0 + c < cols) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] = fmaf(hw_exp2(x[c][i] - stat[c0 + c].x), stat[c0 + c].y, sum[i]);
+        }
+    }
     if (page < 0 || page >= a.c.num_pages) continue;
     float* const sp = a.c.score + page_row(a.c, page, ck.h) + (r & mask);
-    mma_f32x4_t old;
     if (r + 4 <= end) {
-      old = *reinterpret_cast<const mma_f32x4_t*>(sp);
-    } else {
+      mma_f32x4_t old = *reinterpret_cast<const mma_f32x4_t*>(sp);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) old[i] = r + i < end ? sp[i] : 0.0f;
-    }
-    mma_f32x4_t sum = mma_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int g = 0; g < kMaxG; ++g)
-      if (g < G) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = fmaf(hw_exp2(x[g][i] - stat[g].x), stat[g].y, sum[i]);
-      }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) old[i] = fmaf(a.gamma, old[i], sum[i]);
-    if (r + 4 <= end) {
+      for (int i = 0; i < 4; ++i) old[i] = fmaf(a.gamma, old[i], sum[i]);
       *reinterpret_cast<mma_f32x4_t*>(sp) = old;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (r + i < end) sp[i] = old[i];
+        if (r + i < end) sp[i] = fmaf(a.gamma, sp[i], sum[i]);
     }
   }
 }
@@ -548,14 +590,15 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(PagedAttnArgs a, DecWs
 }
 
 // ---------------------------------------------------------------------------
-// Longer queries
+// More columns
 // ---------------------------------------------------------------------------
 constexpr int kTileWaves = 4;     // of a block, 32 columns each
 constexpr int kTileThreads = kWave * kTileWaves;
 constexpr int kTileCols = 32 * kTileWaves;
 constexpr int kKeyStep = 64;      // keys of a step
 constexpr int kLeastKeys = 512;   // of a key range
-constexpr int kRanges = 256;      // blocks that the ranges aim at
+constexpr int kChip = 256;        // CUs
+constexpr int kLongRange = 2048;  // keys from which on two blocks a CU are aimed at
 constexpr int kMaxSplit = 64;     // ranges of a tile
 constexpr float kLag = 8.0f;      // of a running maximum, base 2
 constexpr int kPlanThreads = 1024;
@@ -569,7 +612,7 @@ struct PlanHead {
 constexpr int kSeedWide = 256, kSeedNarrow = 64, kSeedFill = 512;
 constexpr int kSeedGrid = 1024;  // seeding blocks launched, at most
 // One tile and key range, or (splits) one tile with several ranges, or one
-// chunk of a sequence with one query.
+// chunk of a sequence with few columns.
 constexpr int kNoTile = -1, kChunkItem = -2;
 struct PlanItem {
   int b, tile;
@@ -638,7 +681,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   __shared__ int scan_tmp[8][kPlanThreads / kWave];
   __shared__ float sum_tmp[kPlanThreads / kWave];
   // By sequence: rows and queries, first entry of its in the three lists,
-  // first partial, steps before it (one query), keys of a range.
+  // first partial, steps before it (few columns), keys of a range.
   __shared__ int rows_of[kPlanThreads], queries_of[kPlanThreads], item0[kPlanThreads], split0[kPlanThreads];
   __shared__ int seed0[kPlanThreads], slot0[kPlanThreads], steps0[kPlanThreads], keys_of[kPlanThreads];
   __shared__ int hist[kBuckets];
@@ -651,24 +694,27 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   }
   rows_of[tid] = s.n;
   queries_of[tid] = s.ql;
-  const int tiles = s.ql > 1 ? tile_count(s.ql * a.G) : 0;
-  const int steps = s.ql == 1 ? (s.n + kDecStep - 1) / kDecStep : 0;
-  const int wide_seeds = s.ql > 1 ? (s.n + kSeedWide - 1) / kSeedWide : 0;
+  const bool few = few_cols(a, s.ql), many = s.ql > 0 && !few;
+  const int tiles = many ? tile_count(s.ql * a.G) : 0;
+  const int steps = few ? (s.n + kDecStep - 1) / kDecStep : 0;
+  const int wide_seeds = many ? (s.n + kSeedWide - 1) / kSeedWide : 0;
   int v1[2] = {steps, wide_seeds}, t1[2];
   scan_all<2>(v1, t1, scan_tmp);
   steps0[tid] = v1[0];
   const int chunks = dec_chunks(steps, dec_chunk_steps((long long)t1[0] * a.c.HK));
   const float work = sum_all((float)tiles * (float)s.n, sum_tmp) * (float)a.c.HK;
-  // Ranges of like length, about kRanges blocks in all: one block a CU keeps it
-  // two thirds as busy as two do, and a tile that is not cut needs no joining.
-  const float want = fmaxf((float)kLeastKeys, work / (float)kRanges);
+  // Ranges of like length: two blocks a CU, if the ranges are long (512 queries
+  // over 32768 rows: 307 us against 370 with one); else one, for a tile that is
+  // not cut needs no joining (two prompts of 500 queries over 1700 rows beside
+  // 30 decoding users: 131 us against 156 with two).
+  const float want = fmaxf(fmaxf((float)kLeastKeys, work / (2.0f * kChip)), fminf(work / kChip, (float)kLongRange));
   const int ranges = max(1, min(kMaxSplit, (int)((float)s.n / want + 0.5f)));
   const int keys = (int)((((long long)s.n + ranges - 1) / ranges + kKeyStep - 1) / kKeyStep * kKeyStep);
   if (tid < a.c.B) ws.keys[tid] = keys;
   keys_of[tid] = keys;
   const bool wide = (long long)t1[1] * a.c.HK >= kSeedFill;
   const int seed_keys = wide ? kSeedWide : kSeedNarrow;
-  const int seed_blocks = !(a.gamma > 0.0f) || s.ql <= 1 ? 0 : (s.n + seed_keys - 1) / seed_keys;
+  const int seed_blocks = !(a.gamma > 0.0f) || !many ? 0 : (s.n + seed_keys - 1) / seed_keys;
   int v2[5] = {tiles * ranges + chunks, ranges > 1 ? tiles : 0, ranges > 1 ? tiles * ranges : 0, chunks, seed_blocks}, t2[5];
   scan_all<5>(v2, t2, scan_tmp);
   const float count = sum_all((float)tiles * (float)ranges + (float)chunks, sum_tmp);  // also where t2[0] would not hold it
@@ -702,7 +748,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
     const int n = rows_of[b], ql = queries_of[b];
     const int mine = (b + 1 < kPlanThreads ? item0[b + 1] : items) - item0[b];
     it.b = b;
-    if (ql == 1) {
+    if (few_cols(a, ql)) {
       it.tile = kChunkItem;
       it.range = (i - item0[b]) | mine << 8;
       it.slot = slot0[b];
@@ -820,18 +866,19 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
   const int b = it.b, G = a.G, HQ = a.c.HQ;
   const AttnSeq sq = attn_seq(a, b);
   if (it.tile == kChunkItem) {
-    __shared__ float2 wave_ml[kNumWaves][kMaxG];
+    __shared__ float2 wave_ml[kNumWaves][kFewCols];
     DecChunk ck;
     ck.b = b;
     ck.h = h;
     ck.c = it.range & 255;
     ck.nch = it.range >> 8;
     ck.n = sq.n;
+    ck.ql = sq.ql;
     ck.first = it.slot * a.c.HK + h * ck.nch;
     ck.row0 = ((long long)it.steps0 * a.c.HK + (long long)h * ((sq.n + kDecStep - 1) / kDecStep)) * kDecStep;
     ck.q0 = sq.q0;
     static_assert(Cfg::KTILE >= DecCfg<D>::VTILE && kTileThreads == kThreads, "a wave's tile fits a K tile");
-    decode_chunk<T, D, kCap>(a, dec, ck, ck.first + ck.c,
+    decode_chunk<T, D, kCap, false>(a, dec, ck, ck.first + ck.c,
                              [&](int v) { return v & 2 ? (v & 1 ? vt1 : vt0) : (v & 1 ? kt1 : kt0); }, wave_ml);
     return;
   }
@@ -1112,9 +1159,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
     for (int x0 = r0 * CH; x0 < r1 * CH; x0 += kWave) {
       const int x = min(x0 + lane, r1 * CH - 1);
       const uint4 v = *reinterpret_cast<const uint4*>(vcur + Cfg::vaddr(x / CH, 16 * (x % CH)));
-      const uint32_t e = M::kExpMask;
-      auto odd = [&](uint32_t u) { return (u & e) == e || ((u >> 16) & e) == e; };
-      unsigned long long hit = __ballot(odd(v.x) || odd(v.y) || odd(v.z) || odd(v.w));
+      unsigned long long hit = __ballot(M::odd(v));
       while (hit) {  // rare
         const int i = (int)__builtin_ctzll(hit);
         apart |= 1ull << (min(x0 + i, r1 * CH - 1) / CH);
@@ -1255,7 +1300,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
 
 // Tiles whose keys were cut (the first `tiles` blocks: entry of the split list
 // and KV head; 16 columns at a time, 16 lanes each), then the segments with
-// one query.
+// few columns.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs ws, DecWs dec, unsigned tiles, int span) {
   if (blockIdx.x >= tiles) {
@@ -1534,16 +1579,17 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
   };
   z.dec_grid = std::min(dec_blocks(steps * HK), steps * HK / kDecLeastSteps) + (long long)B * HK;
   z.dec.logit_rows = std::min(steps * kDecStep, pool_rows + (long long)B * kDecStep) * HK;
-  z.dec.part = (float*)part((size_t)z.dec_grid * dec_part(G, D) * 4);
-  z.dec.logit = (float*)part((size_t)z.dec.logit_rows * G * 4);
-  if (z.max_q > 1) {
+  const int room = room_cols(z.max_q, G);
+  z.dec.part = (float*)part((size_t)z.dec_grid * dec_part(room, D) * 4);
+  z.dec.logit = (float*)part((size_t)z.dec.logit_rows * room * 4);
+  if (z.max_q > kFewCols / G) {
     // Every sequence with queries rounds up to whole tiles.
     z.tiles = q_rows * G / kTileCols + std::min<int64_t>(B, q_rows);
-    z.items = z.tiles + kRanges / HK + 1 + z.dec_grid / HK + 1;
-    z.slots = z.max_kv <= kLeastKeys ? 0 : std::min<long long>(2LL * kRanges / HK + 2, z.tiles * std::min<long long>(kMaxSplit, (z.max_kv + kLeastKeys - 1) / kLeastKeys));
+    z.items = z.tiles + 2 * kChip / HK + 1 + z.dec_grid / HK + 1;
+    z.slots = z.max_kv <= kLeastKeys ? 0 : std::min<long long>(4LL * kChip / HK + 2, z.tiles * std::min<long long>(kMaxSplit, (z.max_kv + kLeastKeys - 1) / kLeastKeys));
     z.tile.max_items = (int)std::min(z.items, 0x7fffffffLL);
     z.tile.max_slots = (int)z.slots;
-    // Key blocks of sequences with several queries; narrow ones only where the
+    // Key blocks of sequences with many columns; narrow ones only where the
     // wide ones are fewer than kSeedFill, four to a wide one at most.
     const long long wide = std::min<int64_t>(B, q_rows / 2) * ((z.max_kv + kSeedWide - 1LL) / kSeedWide);
     const long long seeds = std::max(wide, std::min(4 * wide, 4LL * kSeedFill / HK + 4));
@@ -1573,8 +1619,9 @@ unsigned finish_blocks(const PagedAttnArgs& a, int& span) {
 }
 
 template <typename T, int D, bool kCap, int R>
-lethe_status launch_one_query(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
-  hipLaunchKernelGGL((decode_kernel<T, D, kCap, R>), dim3((unsigned)z.dec_grid), dim3(kThreads), 0, s, a, z.dec);
+lethe_status launch_few(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
+  const auto kernel = z.max_q <= 1 ? decode_kernel<T, D, kCap, R, true> : decode_kernel<T, D, kCap, R, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)z.dec_grid), dim3(kThreads), 0, s, a, z.dec);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   int span;
   const unsigned y = finish_blocks(a, span);
@@ -1584,7 +1631,7 @@ lethe_status launch_one_query(const PagedAttnArgs& a, const Sizes& z, hipStream_
 
 template <typename T, int D, bool kCap, int R>
 lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
-  if (z.max_q <= 1) return launch_one_query<T, D, kCap, R>(a, z, s);
+  if (z.max_q <= kFewCols / a.G) return launch_few<T, D, kCap, R>(a, z, s);
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, z.tile);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kTileThreads), 0, s, a, z.tile,

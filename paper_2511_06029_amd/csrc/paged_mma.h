@@ -13,6 +13,12 @@ typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_cvoid;
 
+// Whether a 16-bit half of v has all bits of the exponent e.
+__device__ inline bool mma_odd(const uint4& v, uint32_t e) {
+  auto odd = [&](uint32_t u) { return (u & e) == e || ((u >> 16) & e) == e; };
+  return odd(v.x) || odd(v.y) || odd(v.z) || odd(v.w);
+}
+
 template <typename T>
 struct Mma;
 
@@ -21,7 +27,8 @@ struct Mma<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 x4 __attribute__((ext_vector_type(4)));
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));
-  static constexpr uint32_t kExpMask = 0x7f80u;  // exponent of an infinity or NaN
+  // Whether one of eight elements is an infinity or NaN.
+  static __device__ inline bool odd(const uint4& v) { return mma_odd(v, 0x7f80u); }
   static __device__ inline mma_f32x4_t mma16(x8 a, x8 b, mma_f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -38,7 +45,7 @@ struct Mma<_Float16> {
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
   typedef _Float16 x4 __attribute__((ext_vector_type(4)));
   typedef _Float16 x2 __attribute__((ext_vector_type(2)));
-  static constexpr uint32_t kExpMask = 0x7c00u;
+  static __device__ inline bool odd(const uint4& v) { return mma_odd(v, 0x7c00u); }
   static __device__ inline mma_f32x4_t mma16(x8 a, x8 b, mma_f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }

@@ -101,6 +101,23 @@ def test_one_query_over_long_rows():
 
 
 @pytest.mark.parametrize("HQ,HK,D,dtype,page", [
+    (2, 2, 64, "bf16", 16), (8, 4, 128, "f16", 32), (9, 3, 128, "bf16", 16), (16, 4, 64, "f16", 64),
+    (5, 1, 64, "f16", 16), (6, 1, 128, "bf16", 128), (14, 2, 64, "bf16", 512), (8, 1, 128, "f16", 16)])
+@pytest.mark.parametrize("gamma,cap", [(0.0, 0.0), (1.0, 0.0), (0.9, 5.0)])
+def test_few_columns(HQ, HK, D, dtype, page, gamma, cap):
+    """Every number of queries whose columns (queries times group) number 16 at most, none among them."""
+    most = 16 * HK // HQ
+    q_lens = [min(n, 1 + i % most) if i % 5 else 0 for i, n in enumerate(EDGES)]
+    q_lens[-1] = most
+    run(EDGES, q_lens, HQ, HK, D, dtype, page, gamma, cap, gap=1)
+
+
+def test_few_columns_over_long_rows():
+    run([40000, 3, 9001], [2, 2, 1], 8, 1, 128, "bf16", 16, 0.99, seed=3)
+    run([12000], [16], 4, 4, 64, "f16", 64, 1.0, seed=4)
+
+
+@pytest.mark.parametrize("HQ,HK,D,dtype,page", [
     (2, 2, 64, "bf16", 16), (6, 3, 128, "f16", 32), (9, 3, 128, "bf16", 16), (16, 4, 128, "bf16", 64),
     (5, 1, 64, "f16", 16), (6, 1, 128, "bf16", 128), (14, 2, 64, "bf16", 512), (8, 1, 128, "f16", 16)])
 @pytest.mark.parametrize("gamma,cap", [(0.0, 0.0), (1.0, 0.0), (0.9, 5.0)])
@@ -127,7 +144,7 @@ def test_given_scale_and_large_logits():
     run([333, 50], [60, 3], 4, 2, 128, scale=1.5, gamma=1.0)
 
 
-@pytest.mark.parametrize("q_lens", [[1, 1], [5, 40]])
+@pytest.mark.parametrize("q_lens", [[1, 1], [4, 3], [5, 40]])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_values_that_no_query_attends_stay_out(q_lens, dtype):
     """NaN and infinities in later rows reach the queries that attend them and no others."""
@@ -142,7 +159,7 @@ def test_values_that_no_query_attends_stay_out(q_lens, dtype):
         if q_lens[b] > 1:  # only the last queries attend these
             V[0, n - 1] = float("inf")
             V[1, n - 2, 5] = float("nan")
-            V[1, n - 3, 7] = float("-inf")
+            V[1, n - 3, 7] = float("-inf")  # with three queries, every one of them attends this
         pool.put(0, b, K, V, s, torch.arange(n).expand(HK, n))
         new.append((K, V, s))
     out = torch.zeros_like(q)
@@ -152,7 +169,7 @@ def test_values_that_no_query_attends_stay_out(q_lens, dtype):
     check(pool, new, q, q_start, q_lens, out, 0.9, 1 / math.sqrt(D), 0.0)
 
 
-@pytest.mark.parametrize("q_lens", [[1, 1, 1], [3, 30, 1]])
+@pytest.mark.parametrize("q_lens", [[1, 1, 1], [3, 8, 1], [3, 30, 1]])
 def test_rows_on_pages_out_of_range_are_not_attended(q_lens):
     HQ, HK, D, lens = 4, 2, 64, [100, 77, 20]
     pool, rows, g = filled(lens, HQ, HK, D, "bf16", 16, 12)
