@@ -596,10 +596,13 @@ constexpr int kTileWaves = 4;     // of a block, 32 columns each
 constexpr int kTileThreads = kWave * kTileWaves;
 constexpr int kTileCols = 32 * kTileWaves;
 constexpr int kKeyStep = 64;      // keys of a step
-constexpr int kLeastKeys = 512;   // of a key range
+// Keys of a range at least: 3 sequences of 80 queries over 1200 rows take 25.5 us,
+// 29.7 with 512 and 23.6 with 128; 66 of 9 over 370 62.6 and 65.4 with 128.
+constexpr int kLeastKeys = 256;
 constexpr int kChip = 256;        // CUs
 constexpr int kLongRange = 2048;  // keys from which on two blocks a CU are aimed at
 constexpr int kMaxSplit = 64;     // ranges of a tile
+constexpr int kJoinCols = 16;     // columns of a joining block
 constexpr float kLag = 8.0f;      // of a running maximum, base 2
 constexpr int kPlanThreads = 1024;
 constexpr int kBuckets = 1024;
@@ -777,8 +780,16 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
     return (int)(((long long)ql * a.G + 31) / 32 - (long long)max(0, x.y * seed_keys - (n - ql)) * a.G / 32);
   };
   // A list's entries, longest first (the order within a bucket does not
-  // matter).  A thread's only entry is formed once.
+  // matter), unless each has a CU of its own.  A thread's only entry is formed
+  // once.
   auto emit = [&](int count, const auto& entry, const auto& store) {
+    if ((long long)count * a.c.HK <= kChip) {
+      for (int i = tid; i < count; i += kPlanThreads) {
+        entry(i);
+        store(i);
+      }
+      return;
+    }
     hist[tid] = 0;
     __syncthreads();
     int bin = 0;
@@ -1298,9 +1309,11 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
   if (hh == 0 && a.gamma > 0.0f) ws.stat[orow] = make_float2(m, inv);
 }
 
-// Tiles whose keys were cut (the first `tiles` blocks: entry of the split list
-// and KV head; 16 columns at a time, 16 lanes each), then the segments with
-// few columns.
+// Tiles whose keys were cut (the first `tiles` blocks: entry of the split list,
+// KV head and kJoinCols columns, 16 lanes each), then the segments with few
+// columns.  Few bytes and a chain of reads: a lane reads the statistics of
+// every 16th range, and the outputs of eight ranges are asked for at once (16
+// queries over 60000 rows: 64 us less than with one range after the other).
 template <typename T, int D, int R>
 __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs ws, DecWs dec, unsigned tiles, int span) {
   if (blockIdx.x >= tiles) {
@@ -1308,46 +1321,72 @@ __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs 
     finish_segment<T, D, R>(a, dec, span, (int)(i % segs), i / segs);
     return;
   }
-  const int entry = blockIdx.x / a.c.HK, h = blockIdx.x % a.c.HK, G = a.G;
+  const int unit = blockIdx.x / (kTileCols / kJoinCols), G = a.G;
+  const int entry = unit / a.c.HK, h = unit % a.c.HK;
   if (entry >= ws.head->splits) return;
   const PlanItem it = ws.splits[entry];
   const AttnSeq sq = attn_seq(a, it.b);
   constexpr int EL = D / 16;  // dims of a lane
-  const int sub = threadIdx.x / 16, x = threadIdx.x % 16;
-  for (int c = sub; c < kTileCols; c += kThreads / 16) {
-    const int col = kTileCols * it.tile + c;
-    if (col >= sq.ql * G) break;
-    const long long p0 = ((long long)it.slot * a.c.HK + h) * kTileCols + c;
-    const long long ps = (long long)a.c.HK * kTileCols;
-    float m = kNegBig;
-    for (int r = 0; r < it.range; ++r) m = fmaxf(m, ws.part_ml[p0 + r * ps].x);
-    float l = 0.0f, o[EL];
+  constexpr int ML = kMaxSplit / 16;
+  const int x = threadIdx.x % 16, c = kJoinCols * (blockIdx.x % (kTileCols / kJoinCols)) + threadIdx.x / 16;
+  const int col = kTileCols * it.tile + c;
+  if (col >= sq.ql * G) return;  // whole groups of 16 lanes
+  const long long p0 = ((long long)it.slot * a.c.HK + h) * kTileCols + c;
+  const long long ps = (long long)a.c.HK * kTileCols;
+  float2 ml[ML];
+  float m = kNegBig;
 #pragma unroll
-    for (int e = 0; e < EL; ++e) o[e] = 0.0f;
-    for (int r = 0; r < it.range; ++r) {
-      const float2 ml = ws.part_ml[p0 + r * ps];
-      const float f = hw_exp2(ml.x - m);
-      l = fmaf(f, ml.y, l);
-      const float4* const po = reinterpret_cast<const float4*>(ws.part_o + (p0 + r * ps) * D);
+  for (int k = 0; k < ML; ++k) {
+    const int r = 16 * k + x;
+    ml[k] = r < it.range ? ws.part_ml[p0 + r * ps] : make_float2(kNegBig, 0.0f);
+    m = fmaxf(m, ml[k].x);
+  }
 #pragma unroll
-      for (int e = 0; e < EL; e += 4) {
-        const float4 v = po[x + 4 * e];
-        o[e] = fmaf(f, v.x, o[e]);
-        o[e + 1] = fmaf(f, v.y, o[e + 1]);
-        o[e + 2] = fmaf(f, v.z, o[e + 2]);
-        o[e + 3] = fmaf(f, v.w, o[e + 3]);
+  for (int k = 8; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+  float l = 0.0f, f[ML];
+#pragma unroll
+  for (int k = 0; k < ML; ++k) {
+    f[k] = hw_exp2(ml[k].x - m);
+    l = fmaf(f[k], ml[k].y, l);
+  }
+  l = group_sum<16>(l);
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  float o[EL];
+#pragma unroll
+  for (int e = 0; e < EL; ++e) o[e] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < ML; ++k)
+    for (int r0 = 16 * k; r0 < min(it.range, 16 * k + 16); r0 += 8) {
+      float4 v[8][EL / 4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4* const po = reinterpret_cast<const float4*>(ws.part_o + (p0 + min(r0 + i, it.range - 1) * ps) * D);
+#pragma unroll
+        for (int e = 0; e < EL / 4; ++e) v[i][e] = po[x + 16 * e];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float g = __shfl(f[k], r0 % 16 + i, 16);
+        if (r0 + i < it.range) {
+#pragma unroll
+          for (int e = 0; e < EL / 4; ++e) {
+            o[4 * e] = fmaf(g, v[i][e].x, o[4 * e]);
+            o[4 * e + 1] = fmaf(g, v[i][e].y, o[4 * e + 1]);
+            o[4 * e + 2] = fmaf(g, v[i][e].z, o[4 * e + 2]);
+            o[4 * e + 3] = fmaf(g, v[i][e].w, o[4 * e + 3]);
+          }
+        }
       }
     }
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    const long long orow = (sq.q0 + col / G) * a.c.HQ + h * G + col % G;
-    typedef typename Mma<T>::x4 x4;
+  const int query = query_of(a, col);
+  const long long orow = (sq.q0 + query) * a.c.HQ + h * G + col - query * G;
+  typedef typename Mma<T>::x4 x4;
 #pragma unroll
-    for (int e = 0; e < EL; e += 4) {
-      const mma_f32x4_t f = mma_f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]} * inv;
-      reinterpret_cast<x4*>((T*)a.out + orow * D)[x + 4 * e] = __builtin_convertvector(f, x4);
-    }
-    if (x == 0 && a.gamma > 0.0f) ws.stat[orow] = make_float2(m, inv);
+  for (int e = 0; e < EL / 4; ++e) {
+    const mma_f32x4_t y = mma_f32x4_t{o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]} * inv;
+    reinterpret_cast<x4*>((T*)a.out + orow * D)[x + 16 * e] = __builtin_convertvector(y, x4);
   }
+  if (x == 0 && a.gamma > 0.0f) ws.stat[orow] = make_float2(m, inv);
 }
 
 // Second pass, key-major.  A block is KW waves of 32 NS keys each times IG
@@ -1640,7 +1679,7 @@ lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) 
   // A cut tile has two slots at least.
   int span;
   const unsigned y = finish_blocks(a, span);
-  const unsigned tiles = (unsigned)(std::min(z.tiles, z.slots / 2) * a.c.HK);
+  const unsigned tiles = (unsigned)(std::min(z.tiles, z.slots / 2) * a.c.HK * (kTileCols / kJoinCols));
   hipLaunchKernelGGL((join_kernel<T, D, R>), dim3(tiles + (unsigned)(a.c.B * a.c.HK) * y), dim3(kThreads), 0, s, a, z.tile,
                      z.dec, tiles, span);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;

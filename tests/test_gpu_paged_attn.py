@@ -134,6 +134,11 @@ def test_few_queries_over_long_rows():
     run([20000], [2], 4, 1, 64, "f16", 64, 0.9, cap=20.0, seed=6)
 
 
+def test_as_many_key_ranges_as_a_tile_can_have():
+    run([20000], [6], 4, 1, 64, "f16", 64, 0.9, cap=20.0, seed=7)
+    run([4700, 2100, 300], [40, 9, 6], 4, 1, 128, "bf16", 16, 1.0, seed=8)
+
+
 def test_layers_and_loose_bounds():
     run([100, 17], [1, 1], 4, 2, 64, layers=3, layer=2, loose=True)
     run([100, 17], [40, 1], 4, 2, 64, layers=3, layer=1, loose=True)
