@@ -615,21 +615,29 @@ struct PlanHead {
 constexpr int kSeedWide = 256, kSeedNarrow = 64, kSeedFill = 512;
 constexpr int kSeedGrid = 1024;  // seeding blocks launched, at most
 // One tile and key range, or (splits) one tile with several ranges, or one
-// chunk of a sequence with few columns.
+// chunk of a sequence with few columns.  An entry has its sequence's sizes, so
+// that the block that takes it waits for one read before those of its rows.
 constexpr int kNoTile = -1, kChunkItem = -2;
-struct PlanItem {
+struct alignas(16) PlanItem {
   int b, tile;
   int range;   // in the split list, how many; of a chunk, its number and, from bit 8 on, how many the segment has
   int slot;    // of its partial, -1: the only range; of a chunk, the chunks of one head before the sequence
   int steps0;  // of a chunk, the steps of one head before the sequence
+  int keys;    // of a range
+  int n, ql;
+  long long q0;
+};
+struct alignas(16) PlanSeed {
+  int b, block;  // of seed keys
+  int n, ql;
+  long long q0;
 };
 
 struct TileWs {
   PlanHead* head;
-  int32_t* keys;     // [B] keys of a range
   PlanItem* items;
   PlanItem* splits;
-  int2* seeds;       // sequence and key block
+  PlanSeed* seeds;
   float2* stat;      // [q_rows][HQ] max (base 2), 1 / sum
   float2* part_ml;   // [slots][HK][kTileCols]
   float* part_o;     // [slots][HK][kTileCols][D]
@@ -687,6 +695,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   // first partial, steps before it (few columns), keys of a range.
   __shared__ int rows_of[kPlanThreads], queries_of[kPlanThreads], item0[kPlanThreads], split0[kPlanThreads];
   __shared__ int seed0[kPlanThreads], slot0[kPlanThreads], steps0[kPlanThreads], keys_of[kPlanThreads];
+  __shared__ long long query0[kPlanThreads];
   __shared__ int hist[kBuckets];
   const int tid = threadIdx.x;
   AttnSeq s{0, 0, 0, true};
@@ -697,6 +706,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   }
   rows_of[tid] = s.n;
   queries_of[tid] = s.ql;
+  query0[tid] = s.q0;
   const bool few = few_cols(a, s.ql), many = s.ql > 0 && !few;
   const int tiles = many ? tile_count(s.ql * a.G) : 0;
   const int steps = few ? (s.n + kDecStep - 1) / kDecStep : 0;
@@ -713,7 +723,6 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   const float want = fmaxf(fmaxf((float)kLeastKeys, work / (2.0f * kChip)), fminf(work / kChip, (float)kLongRange));
   const int ranges = max(1, min(kMaxSplit, (int)((float)s.n / want + 0.5f)));
   const int keys = (int)((((long long)s.n + ranges - 1) / ranges + kKeyStep - 1) / kKeyStep * kKeyStep);
-  if (tid < a.c.B) ws.keys[tid] = keys;
   keys_of[tid] = keys;
   const bool wide = (long long)t1[1] * a.c.HK >= kSeedFill;
   const int seed_keys = wide ? kSeedWide : kSeedNarrow;
@@ -751,6 +760,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
     const int n = rows_of[b], ql = queries_of[b];
     const int mine = (b + 1 < kPlanThreads ? item0[b + 1] : items) - item0[b];
     it.b = b;
+    it.n = n;
+    it.ql = ql;
+    it.q0 = query0[b];
+    it.keys = keys_of[b];
     if (few_cols(a, ql)) {
       it.tile = kChunkItem;
       it.range = (i - item0[b]) | mine << 8;
@@ -758,7 +771,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
       it.steps0 = steps0[b];
       return max(n / mine, 1);
     }
-    const int per = keys_of[b];
+    const int per = it.keys;
     const int nr = mine / tile_count(ql * a.G);
     it.steps0 = 0;
     it.tile = (i - item0[b]) / nr;
@@ -767,17 +780,18 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
     const int end = key_end(AttnSeq{n, ql, 0, true}, kTileCols * it.tile + kTileCols - 1, a.G);
     const long long from = (long long)it.range * per;
     if (it.range == 0 && nr > 1) {
-      const PlanItem sp{b, it.tile, (int)((end + per - 1) / per), slot0[b] + it.tile * nr, 0};
+      PlanItem sp = it;
+      sp.range = (int)((end + per - 1) / per);
+      sp.slot = slot0[b] + it.tile * nr;
       ws.splits[split0[b] + it.tile] = sp;
     }
     return from >= end ? 0 : (int)(min((long long)end, from + per) - from);
   };
   // Key block i of the seeding pass and the column tiles it meets.
-  auto seed = [&](int i, int2& x) {
-    x.x = sequence(seed0, i);
-    x.y = i - seed0[x.x];
-    const int n = rows_of[x.x], ql = queries_of[x.x];
-    return (int)(((long long)ql * a.G + 31) / 32 - (long long)max(0, x.y * seed_keys - (n - ql)) * a.G / 32);
+  auto seed = [&](int i, PlanSeed& x) {
+    const int b = sequence(seed0, i);
+    x = PlanSeed{b, i - seed0[b], rows_of[b], queries_of[b], query0[b]};
+    return (int)(((long long)x.ql * a.G + 31) / 32 - (long long)max(0, x.block * seed_keys - (x.n - x.ql)) * a.G / 32);
   };
   // A list's entries, longest first (the order within a bucket does not
   // matter), unless each has a CU of its own.  A thread's only entry is formed
@@ -816,7 +830,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
         return (keyn + kKeyStep - 1) / kKeyStep;
       },
       [&](int at) { ws.items[at] = it; });
-  int2 sd;
+  PlanSeed sd;
   emit(
       seeds, [&](int i) { return seed(i, sd); }, [&](int at) { ws.seeds[at] = sd; });
 }
@@ -871,11 +885,10 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
   const int s = lane & 31;   // column
   const int h = blockIdx.x % a.c.HK;
   const int at = blockIdx.x / a.c.HK;
-  if (at >= ws.head->items) return;
-  const PlanItem it = ws.items[at];
-  if (it.tile == kNoTile) return;
+  const PlanItem it = ws.items[at];  // read beside the list's length
+  if (at >= ws.head->items || it.tile == kNoTile) return;
   const int b = it.b, G = a.G, HQ = a.c.HQ;
-  const AttnSeq sq = attn_seq(a, b);
+  const AttnSeq sq{it.n, it.ql, it.q0, true};
   if (it.tile == kChunkItem) {
     __shared__ float2 wave_ml[kNumWaves][kFewCols];
     DecChunk ck;
@@ -894,10 +907,10 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
     return;
   }
   const int cols = sq.ql * G, first = sq.n - sq.ql;
-  const int ks = it.range * ws.keys[b];
+  const int ks = it.range * it.keys;
   // Keys [ks, kend) of this wave and of the block; rows up to `full` are
   // attended by each of the wave's columns.
-  const int range_end = (int)min((long long)ks + ws.keys[b], (long long)sq.n);
+  const int range_end = (int)min((long long)ks + it.keys, (long long)sq.n);
   const int c0 = kTileCols * it.tile + 32 * w;
   const bool active = c0 < cols;
   const int kend_blk = min(range_end, key_end(sq, kTileCols * it.tile + kTileCols - 1, G));
@@ -1323,9 +1336,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs 
   }
   const int unit = blockIdx.x / (kTileCols / kJoinCols), G = a.G;
   const int entry = unit / a.c.HK, h = unit % a.c.HK;
+  const PlanItem it = ws.splits[entry];  // read beside the list's length
   if (entry >= ws.head->splits) return;
-  const PlanItem it = ws.splits[entry];
-  const AttnSeq sq = attn_seq(a, it.b);
+  const AttnSeq sq{it.n, it.ql, it.q0, true};
   constexpr int EL = D / 16;  // dims of a lane
   constexpr int ML = kMaxSplit / 16;
   const int x = threadIdx.x % 16, c = kJoinCols * (blockIdx.x % (kTileCols / kJoinCols)) + threadIdx.x / 16;
@@ -1400,7 +1413,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs 
 constexpr int kSeedThreads = 512;
 
 template <typename T, int D, bool kCap, int NS, int KW, int IG>
-__device__ inline void seed_block(const PagedAttnArgs& a, const TileWs& ws, int b, int h, int kblk0, char* const buf0,
+__device__ inline void seed_block(const PagedAttnArgs& a, const TileWs& ws, const PlanSeed& sq, int h, int kblk0, char* const buf0,
                                   char* const buf1, float* const sums) {
   using Cfg = TileCfg<D>;
   using M = Mma<T>;
@@ -1415,8 +1428,7 @@ __device__ inline void seed_block(const PagedAttnArgs& a, const TileWs& ws, int 
   const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int kw = w % KW, ig = w / KW;
   const int hh = lane >> 5, s = lane & 31;
-  const AttnSeq sq = attn_seq(a, b);
-  const int G = a.G, HQ = a.c.HQ, cols = sq.ql * G, first = sq.n - sq.ql;
+  const int b = sq.b, G = a.G, HQ = a.c.HQ, cols = sq.ql * G, first = sq.n - sq.ql;
   const int j0w = kblk0 + 32 * NS * kw;
 
   // This wave's keys as the A operand (row 32 t + s, dims 16 kk + 8 hh ..).
@@ -1576,12 +1588,12 @@ __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(2)
   static_assert(2 * kSeedWide >= 4 * kSeedNarrow, "both forms' sums fit");
   const PlanHead head = *ws.head;
   for (int i = blockIdx.x; i < head.seeds * a.c.HK; i += gridDim.x) {
-    const int2 x = ws.seeds[i / a.c.HK];
+    const PlanSeed x = ws.seeds[i / a.c.HK];
     const int h = i % a.c.HK;
     if (head.wide)
-      seed_block<T, D, kCap, 2, 4, 2>(a, ws, x.x, h, x.y * kSeedWide, buf0, buf1, sums);
+      seed_block<T, D, kCap, 2, 4, 2>(a, ws, x, h, x.block * kSeedWide, buf0, buf1, sums);
     else
-      seed_block<T, D, kCap, 1, 2, 4>(a, ws, x.x, h, x.y * kSeedNarrow, buf0, buf1, sums);
+      seed_block<T, D, kCap, 1, 2, 4>(a, ws, x, h, x.block * kSeedNarrow, buf0, buf1, sums);
     __syncthreads();  // the buffers are free
   }
 }
@@ -1635,10 +1647,9 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
     if (seeds * HK > 0x7fffffffLL) return false;
     z.tile.max_seeds = (int)seeds;
     z.tile.head = (PlanHead*)part(sizeof(PlanHead));
-    z.tile.keys = (int32_t*)part((size_t)B * 4);
     z.tile.items = (PlanItem*)part((size_t)z.items * sizeof(PlanItem));
     z.tile.splits = (PlanItem*)part((size_t)z.items * sizeof(PlanItem));
-    z.tile.seeds = (int2*)part((size_t)seeds * sizeof(int2));
+    z.tile.seeds = (PlanSeed*)part((size_t)seeds * sizeof(PlanSeed));
     z.tile.stat = (float2*)part((size_t)q_rows * HQ * sizeof(float2));
     z.tile.part_ml = (float2*)part((size_t)z.slots * HK * kTileCols * sizeof(float2));
     z.tile.part_o = (float*)part((size_t)z.slots * HK * kTileCols * D * 4);
