@@ -604,7 +604,8 @@ lethe_status lethe_paged_append(const lethe_paged_cache* cache, int32_t layer, c
  *  q_start, q_len, q_rows, max_q_len, max_kv_len  as for
  *           lethe_prefill_attn_score; the bounds choose the kernels and size
  *           the workspace.  Row ranges must not overlap.
- *  softmax_scale  > 0, or <= 0 for 1/sqrt(head_dim); softcap >= 0, 0 for none.
+ *  softmax_scale  > 0, or <= 0 for 1/sqrt(head_dim).  softcap 0 .. 1024, 0 for
+ *           none; a capped x is off by up to about softcap * 2^-21.
  *  ws       lethe_paged_attn_workspace_bytes(cache, q_rows, max_q_len,
  *           max_kv_len) bytes, not shared by calls that may run at once.
  * A row on a page out of range is not attended and its score not updated; a

@@ -1,5 +1,6 @@
 // Host side of the paged cache's calls: argument validation, workspace sizing
 // and launch dispatch.  Every check runs before any HIP call.
+#include <float.h>
 #include <math.h>
 
 #include "paged_internal.h"
@@ -54,6 +55,10 @@ PagedView view(const lethe_paged_cache* c, int layer) {
   p.dev_status = c->dev_status;
   return p;
 }
+
+// A capped logit is cap - 2 cap / (1 + exp(2 x / cap)): it is off by a few
+// roundings of cap, whatever its size.
+constexpr float kMaxCap = 1024.0f;
 
 int64_t pool_rows(const lethe_paged_cache* c) { return c->num_pages * c->page_size; }
 
@@ -159,6 +164,7 @@ lethe_status lethe_paged_attn_score(const lethe_paged_cache* c, int32_t layer, c
   if (gamma > 0.0f && (!c->score || !aligned16(c->score))) return LETHE_ERR_INVALID;
   if (isnan(softmax_scale) || isinf(softmax_scale)) return LETHE_ERR_INVALID;
   if (!(softcap >= 0.0f) || isinf(softcap)) return LETHE_ERR_INVALID;
+  if (softcap > kMaxCap) return LETHE_ERR_UNSUPPORTED;
   st = check_bounds(q_rows, max_q_len);
   if (st != LETHE_OK) return st;
   if (ws_bytes < lethe_paged_attn_workspace_bytes(c, q_rows, max_q_len, max_kv_len)) return LETHE_ERR_WORKSPACE;
@@ -175,7 +181,8 @@ lethe_status lethe_paged_attn_score(const lethe_paged_cache* c, int32_t layer, c
   a.G = c->num_q_heads / c->num_kv_heads;
   a.g_magic = a.G > 1 ? (uint32_t)((0xffffffffULL + a.G) / a.G) : 0u;
   a.scale_log2 = scale * kLog2e;
-  a.cap_in = softcap > 0.0f ? 2.0f * scale * kLog2e / softcap : 0.0f;
+  // Finite, so that a product of 0 stays 0 under the smallest caps.
+  a.cap_in = softcap > 0.0f ? fminf(2.0f * scale * kLog2e / softcap, FLT_MAX) : 0.0f;
   a.cap_log2 = softcap * kLog2e;
   a.gamma = gamma;
   a.out = out;

@@ -1628,6 +1628,8 @@ bool sizes(Sizes& z, int64_t q_rows, int max_q, long long max_kv, int B, int HQ,
     p += align_up(bytes, 256);
     return at;
   };
+  // Threads of a launch stay below 2^32 (the largest are the joining ones).
+  if ((4LL * B * HK + 8LL * HK + 32768) * kThreads > 0xffffffffLL) return false;
   z.dec_grid = std::min(dec_blocks(steps * HK), steps * HK / kDecLeastSteps) + (long long)B * HK;
   z.dec.logit_rows = std::min(steps * kDecStep, pool_rows + (long long)B * kDecStep) * HK;
   const int room = room_cols(z.max_q, G);

@@ -305,7 +305,15 @@ def _row_stride(fn, t, heads, dim, dtype):
     return row if rows > 1 else heads * dim
 
 
+def _check_place(fn, cache, *tensors):
+    """Every tensor (None: not given) lies on the cache's device."""
+    for t in tensors:
+        if t is not None and t.device != cache.device:
+            raise LetheError(fn, ERR_INVALID)
+
+
 def _check_batch(fn, cache, q_start, q_len):
+    _check_place(fn, cache, q_start, q_len)
     if (q_start.dtype != cache.torch.int64 or q_len.dtype != cache.torch.int32 or q_start.numel() != cache.B or
             q_len.numel() != cache.B or not q_start.is_contiguous() or not q_len.is_contiguous()):
         raise LetheError(fn, ERR_INVALID)
@@ -345,6 +353,7 @@ def paged_append(cache, layer, q, k_new, v_new, q_start, q_len, max_q_len, rotar
         op = q_out.data_ptr()
     if rotary is not None and rotary.rows != rows:
         raise LetheError(fn, ERR_INVALID)
+    _check_place(fn, cache, q, k_new, v_new, q_out, *(() if rotary is None else (rotary.inv_freq, rotary.axis_pos)))
     _check_batch(fn, cache, q_start, q_len)
     _paged_call(fn, cache, stream, layer, qp, qd, k_new.data_ptr(), kd, v_new.data_ptr(), vd, q_start.data_ptr(),
                 q_len.data_ptr(), rows, max_q_len, None if rotary is None else rotary.ref, op)
@@ -360,6 +369,9 @@ def paged_attn_score(cache, layer, q, q_start, q_len, max_q_len, max_kv_len, gam
     for t in (q, out):
         if t.dtype != cache.tdtype or not t.is_contiguous() or t.shape != (rows, cache.HQ, cache.D):
             raise LetheError(fn, ERR_INVALID)
+    _check_place(fn, cache, q, out, ws)
+    if not ws.is_contiguous():
+        raise LetheError(fn, ERR_INVALID)
     _check_batch(fn, cache, q_start, q_len)
     _paged_call(fn, cache, stream, layer, q.data_ptr(), q_start.data_ptr(), q_len.data_ptr(), rows, max_q_len,
                 max_kv_len, gamma, softmax_scale, softcap, out.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
@@ -370,6 +382,9 @@ def paged_evict(cache, budget, recent, sink, ws, max_kv_len=None, stream=None):
     cache.evict_workspace; max_kv_len: an upper bound of the lengths (default: the tables' room)."""
     fn = "lethe_paged_evict"
     if budget.dtype != cache.torch.int32 or not budget.is_contiguous() or budget.shape != (cache.B, cache.L):
+        raise LetheError(fn, ERR_INVALID)
+    _check_place(fn, cache, budget, ws)
+    if not ws.is_contiguous():
         raise LetheError(fn, ERR_INVALID)
     _paged_call(fn, cache, stream, budget.data_ptr(), recent, sink, 0x7fffffff if max_kv_len is None else max_kv_len,
                 ws.data_ptr(), ws.numel() * ws.element_size())

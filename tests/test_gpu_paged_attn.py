@@ -139,6 +139,12 @@ def test_as_many_key_ranges_as_a_tile_can_have():
     run([4700, 2100, 300], [40, 9, 6], 4, 1, 128, "bf16", 16, 1.0, seed=8)
 
 
+@pytest.mark.parametrize("cap", [1e-38, 1e-6, 1024.0])
+def test_smallest_and_largest_caps(cap):
+    run([100, 65], [1, 1], 4, 2, 64, cap=cap)
+    run([100, 65], [30, 1], 4, 2, 64, "f16", cap=cap)
+
+
 def test_layers_and_loose_bounds():
     run([100, 17], [1, 1], 4, 2, 64, layers=3, layer=2, loose=True)
     run([100, 17], [40, 1], 4, 2, 64, layers=3, layer=1, loose=True)

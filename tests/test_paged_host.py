@@ -90,6 +90,7 @@ def test_attention_arguments():
                dict(kv=-1), dict(gamma=-0.1), dict(gamma=1.1), dict(gamma=math.nan), dict(scale=math.nan),
                dict(scale=math.inf), dict(cap=-1.0), dict(cap=math.nan), dict(cap=math.inf)):
         assert attn(c, **kw) == L.ERR_INVALID, kw
+    assert attn(c, cap=1024.5) == L.ERR_UNSUPPORTED and attn(c, cap=1024.0, wsb=0) == L.ERR_WORKSPACE
     assert attn(make(score=None)) == L.ERR_INVALID
     for most in (1, 4):
         need = L.load().lethe_paged_attn_workspace_bytes(ctypes.byref(c), 4, most, 100)
@@ -97,6 +98,8 @@ def test_attention_arguments():
     huge = make(num_seqs=1024, max_pages=1 << 26)
     assert L.load().lethe_paged_attn_workspace_bytes(ctypes.byref(huge), 4, 1, 2 ** 31 - 1) == 0
     assert attn(huge, kv=2 ** 31 - 1) == L.ERR_UNSUPPORTED
+    wide = make(num_seqs=1024, num_q_heads=8192, num_kv_heads=8192)
+    assert L.load().lethe_paged_attn_workspace_bytes(ctypes.byref(wide), 4, 1, 16) == 0
 
 
 def test_eviction_arguments():
@@ -140,6 +143,35 @@ def test_tensors_of_another_shape_or_type():
     with pytest.raises(L.LetheError) as e:
         L.LethePagedCache(c.k, c.v, c.score, c.pos, c.len, c.seen, c.page_table, 18)
     assert e.value.status == L.ERR_UNSUPPORTED
+
+
+def test_tensors_on_another_device():
+    pool = plain.Pool(1, 2, [[20, 20]], 4, 2, 64, "bf16", 16, 1, device="cpu")
+    c = pool.cache
+    bf16, i32, i64 = torch.bfloat16, torch.int32, torch.int64
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    append = [torch.zeros((3, 4, 64), dtype=bf16), torch.zeros((3, 2, 64), dtype=bf16),
+              torch.zeros((3, 2, 64), dtype=bf16), torch.zeros(2, dtype=i64), torch.zeros(2, dtype=i32),
+              torch.zeros(32), torch.zeros((1, 3), dtype=i32), torch.zeros((3, 4, 64), dtype=bf16)]
+    attend = [append[0], append[3], append[4], append[7], ws]
+    prune = [torch.zeros((2, 1), dtype=i32), ws]
+
+    def do_append(q, k, v, start, length, freq, axis, out):
+        L.paged_append(c, 0, q, k, v, start, length, 1, L.Rotary(freq, axis, [32]), out)
+
+    def do_attend(q, start, length, out, w):
+        L.paged_attn_score(c, 0, q, start, length, 1, 20, 1.0, 0.0, 0.0, out, w)
+
+    for fn, tensors in ((do_append, append), (do_attend, attend), (lambda b, w: L.paged_evict(c, b, 0, 0, w), prune)):
+        for i in range(len(tensors)):
+            args = [t.to("meta") if i == j else t for j, t in enumerate(tensors)]
+            with pytest.raises(L.LetheError) as e:
+                fn(*args)
+            assert e.value.status == L.ERR_INVALID
+    for fn in (lambda w: do_attend(*attend[:4], w), lambda w: L.paged_evict(c, prune[0], 0, 0, w)):
+        with pytest.raises(L.LetheError) as e:
+            fn(ws[::2])
+        assert e.value.status == L.ERR_INVALID
 
 
 def test_plain_eviction_is_a_permutation_of_the_rule():
