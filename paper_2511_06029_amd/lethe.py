@@ -325,8 +325,8 @@ def _paged_call(fn, cache, stream, *args):
     if cuda.current_device() != cache.device.index:
         with cuda.device(cache.device):
             return _paged_call(fn, cache, stream, *args)
-    if stream is None:
-        stream = cuda.current_stream().cuda_stream
+    if stream is None:  # the raw handle: a Stream object costs 2.8 us of the 12 that a one-token call takes
+        stream = cache.torch._C._cuda_getCurrentRawStream(cache.device.index)
     elif not isinstance(stream, int):
         stream = stream.cuda_stream
     st = getattr(load(), fn)(cache.ref, *args, stream)
