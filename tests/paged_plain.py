@@ -75,6 +75,12 @@ def rotate(x, axis_pos, inv_freq, sections, adjacent):
     return y, size
 
 
+def rounding(ref, size, dtype):
+    """Half a step of the result; the pair's fp32 products and the angle's fraction (2^-25 of a turn) before it."""
+    fi = torch.finfo(dtype)
+    return fi.eps / 2 * ref.abs() * 1.001 + size * 2.0 ** -20 + fi.smallest_normal * fi.eps / 2
+
+
 def attend(q, K, V, score, gamma, scale, cap):
     """q [ql][HQ][D], K and V [HK][n][D], score [HK][n]: out [ql][HQ][D], new scores [HK][n], and the bounds of their
     errors but for the roundings to the storage type: out's in units of sum p |v|, given with it."""

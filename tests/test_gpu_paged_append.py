@@ -10,12 +10,6 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
-def rounding(ref, size, dtype):
-    """Half a step of the result; the pair's fp32 products and the angle's fraction (2^-25 of a turn) before it."""
-    fi = torch.finfo(dtype)
-    return fi.eps / 2 * ref.abs() * 1.001 + size * 2.0 ** -20 + fi.smallest_normal * fi.eps / 2
-
-
 def batch(lens, first_row=0, gap=0):
     """q_start and q_len of consecutive chunks, `gap` rows of no sequence between them."""
     starts, at = [], first_row
@@ -66,7 +60,7 @@ def test_append(case):
         torch.cuda.synchronize()
         assert int(c.dev_status[0]) == 0
         rot, size = plain.rotate(qkv[:, :HQ + HK], axis_pos, inv_freq, sections, adjacent)
-        tol = rounding(rot, size, T)
+        tol = plain.rounding(rot, size, T)
         written = torch.zeros(c.score.shape, dtype=torch.bool)
         for b in range(B):
             rs = slice(int(q_start[b]), int(q_start[b]) + new[b])
