@@ -7,7 +7,10 @@
 // and cosines once in shared memory, and then copies: an item is 16 elements
 // of one head of one row (two 16-byte pieces, the two halves of eight pairs),
 // neighbouring lanes on neighbouring pieces.  Bytes bound it: each element is
-// read once and written once.
+// read once and written once (8 sequences of 1500 to 2048 rows of 48 heads, 347
+// MB: 77 us, 4.6 TB/s, a large copy reaching 4.8); one row is a chain of four
+// reads (4.6 us).  Eight rows a block share the search and the sines; one a
+// block while the rows do not fill the chip.
 //
 // The angle is a position times a frequency, reduced to a turn's fraction in
 // 64 bits (a position of 10^6 leaves an fp32 product no more than two decimal

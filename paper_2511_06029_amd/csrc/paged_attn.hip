@@ -12,6 +12,8 @@
 //     scores, the rows' logits.
 //  2. finish_kernel: joins a segment's chunks and turns the logits into
 //     weights once the segment's max and sum are known.
+//  128 users over 200 to 12000 rows, 8 KV heads, 1.54 GB: 289 + 28 us, 4.8 TB/s
+//  (256 us without scores, 6.0 TB/s; a read stream reaches 6.2).
 //
 // More columns, bound by the products (sequences with few decode beside them):
 //  1. plan_kernel (one block): cuts every (sequence, 128 columns) into key
@@ -22,6 +24,9 @@
 //  3. join_kernel: where a tile's keys were cut.
 //  4. seed_kernel (with scores): key-major second pass, the columns' final
 //     max and sum at hand, in a fixed order without atomics.
+//  Eight prompts of 2048 rows, 32 query heads: 10 + 365 + 5 + 205 us, the tiles
+//  at 0.76 PFLOP/s; over 32768 rows 1.04 (0.86 capped; a large library product
+//  reaches 1.2).
 #include <algorithm>
 
 #include "paged_internal.h"
