@@ -24,7 +24,7 @@
 //  3. join_kernel: where a tile's keys were cut.
 //  4. seed_kernel (with scores): key-major second pass, the columns' final
 //     max and sum at hand, in a fixed order without atomics.
-//  Eight prompts of 2048 rows, 32 query heads: 10 + 365 + 5 + 205 us, the tiles
+//  Eight prompts of 2048 rows, 32 query heads: 9 + 365 + 5 + 205 us, the tiles
 //  at 0.76 PFLOP/s; over 32768 rows 1.04 (0.86 capped; a large library product
 //  reaches 1.2).
 #include <algorithm>
@@ -609,8 +609,7 @@ constexpr int kLongRange = 2048;  // keys from which on two blocks a CU are aime
 constexpr int kMaxSplit = 64;     // ranges of a tile
 constexpr int kJoinCols = 16;     // columns of a joining block
 constexpr float kLag = 8.0f;      // of a running maximum, base 2
-constexpr int kPlanThreads = 1024;
-constexpr int kBuckets = 1024;
+constexpr int kBuckets = 1024;    // of the lists' order, by length
 
 struct PlanHead {
   int items, splits, seeds;  // entries of the lists
@@ -654,9 +653,9 @@ __device__ inline int tile_count(int cols) { return (cols + kTileCols - 1) / kTi
 __device__ inline int key_end(const AttnSeq& s, int last, int G) { return s.n - s.ql + min(last / G, s.ql - 1) + 1; }
 
 // Exclusive prefix sums of K values a thread and their totals, over a block of
-// kPlanThreads.
-template <int K>
-__device__ inline void scan_all(int (&v)[K], int (&total)[K], int (&tmp)[8][kPlanThreads / kWave]) {
+// NT threads.
+template <int K, int NT>
+__device__ inline void scan_all(int (&v)[K], int (&total)[K], int (&tmp)[8][NT / kWave]) {
   const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
   int own[K];
 #pragma unroll
@@ -670,7 +669,7 @@ __device__ inline void scan_all(int (&v)[K], int (&total)[K], int (&tmp)[8][kPla
   for (int k = 0; k < K; ++k) {
     int before = 0, all = 0;
 #pragma unroll
-    for (int i = 0; i < kPlanThreads / kWave; ++i) {
+    for (int i = 0; i < NT / kWave; ++i) {
       const int x = tmp[k][i];
       before += i < w ? x : 0;
       all += x;
@@ -682,25 +681,30 @@ __device__ inline void scan_all(int (&v)[K], int (&total)[K], int (&tmp)[8][kPla
 }
 
 // Sum of a float over the block, the same for every thread.
-__device__ inline float sum_all(float v, float (&tmp)[kPlanThreads / kWave]) {
+template <int NT>
+__device__ inline float sum_all(float v, float (&tmp)[NT / kWave]) {
   v = group_sum<kWave>(v);
   if ((threadIdx.x & (kWave - 1)) == 0) tmp[threadIdx.x / kWave] = v;
   __syncthreads();
   float all = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kPlanThreads / kWave; ++i) all += tmp[i];
+  for (int i = 0; i < NT / kWave; ++i) all += tmp[i];
   __syncthreads();
   return all;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, TileWs ws) {
-  __shared__ int scan_tmp[8][kPlanThreads / kWave];
-  __shared__ float sum_tmp[kPlanThreads / kWave];
+// NT threads, one a sequence at least: 256 where they are enough (4 chunks of 40
+// to 100 queries 31.7 us, 33.5 with 1024, whose waves each read every wave's
+// partial sums).
+template <int NT>
+__global__ __launch_bounds__(NT) void plan_kernel(PagedAttnArgs a, TileWs ws) {
+  __shared__ int scan_tmp[8][NT / kWave];
+  __shared__ float sum_tmp[NT / kWave];
   // By sequence: rows and queries, first entry of its in the three lists,
   // first partial, steps before it (few columns), keys of a range.
-  __shared__ int rows_of[kPlanThreads], queries_of[kPlanThreads], item0[kPlanThreads], split0[kPlanThreads];
-  __shared__ int seed0[kPlanThreads], slot0[kPlanThreads], steps0[kPlanThreads], keys_of[kPlanThreads];
-  __shared__ long long query0[kPlanThreads];
+  __shared__ int rows_of[NT], queries_of[NT], item0[NT], split0[NT];
+  __shared__ int seed0[NT], slot0[NT], steps0[NT], keys_of[NT];
+  __shared__ long long query0[NT];
   __shared__ int hist[kBuckets];
   const int tid = threadIdx.x;
   AttnSeq s{0, 0, 0, true};
@@ -717,10 +721,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   const int steps = few ? (s.n + kDecStep - 1) / kDecStep : 0;
   const int wide_seeds = many ? (s.n + kSeedWide - 1) / kSeedWide : 0;
   int v1[2] = {steps, wide_seeds}, t1[2];
-  scan_all<2>(v1, t1, scan_tmp);
+  scan_all<2, NT>(v1, t1, scan_tmp);
   steps0[tid] = v1[0];
   const int chunks = dec_chunks(steps, dec_chunk_steps((long long)t1[0] * a.c.HK));
-  const float work = sum_all((float)tiles * (float)s.n, sum_tmp) * (float)a.c.HK;
+  const float work = sum_all<NT>((float)tiles * (float)s.n, sum_tmp) * (float)a.c.HK;
   // Ranges of like length: two blocks a CU, if the ranges are long (512 queries
   // over 32768 rows: 307 us against 370 with one); else one, for a tile that is
   // not cut needs no joining (two prompts of 500 queries over 1700 rows beside
@@ -733,8 +737,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   const int seed_keys = wide ? kSeedWide : kSeedNarrow;
   const int seed_blocks = !(a.gamma > 0.0f) || !many ? 0 : (s.n + seed_keys - 1) / seed_keys;
   int v2[5] = {tiles * ranges + chunks, ranges > 1 ? tiles : 0, ranges > 1 ? tiles * ranges : 0, chunks, seed_blocks}, t2[5];
-  scan_all<5>(v2, t2, scan_tmp);
-  const float count = sum_all((float)tiles * (float)ranges + (float)chunks, sum_tmp);  // also where t2[0] would not hold it
+  scan_all<5, NT>(v2, t2, scan_tmp);
+  const float count = sum_all<NT>((float)tiles * (float)ranges + (float)chunks, sum_tmp);  // also where t2[0] would not hold it
   item0[tid] = v2[0];
   split0[tid] = v2[1];
   slot0[tid] = chunks ? v2[3] : v2[2];
@@ -748,7 +752,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   }
   __syncthreads();
   // The sequence that entry i of a list belongs to (empty ones share a start).
-  auto sequence = [&](const int (&first)[kPlanThreads], int i) {
+  auto sequence = [&](const int (&first)[NT], int i) {
     int lo = 0, hi = a.c.B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
@@ -763,7 +767,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   auto item = [&](int i, PlanItem& it) {
     const int b = sequence(item0, i);
     const int n = rows_of[b], ql = queries_of[b];
-    const int mine = (b + 1 < kPlanThreads ? item0[b + 1] : items) - item0[b];
+    const int mine = (b + 1 < NT ? item0[b + 1] : items) - item0[b];
     it.b = b;
     it.n = n;
     it.ql = ql;
@@ -803,26 +807,37 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PagedAttnArgs a, Til
   // once.
   auto emit = [&](int count, const auto& entry, const auto& store) {
     if ((long long)count * a.c.HK <= kChip) {
-      for (int i = tid; i < count; i += kPlanThreads) {
+      for (int i = tid; i < count; i += NT) {
         entry(i);
         store(i);
       }
       return;
     }
-    hist[tid] = 0;
+    constexpr int PER = kBuckets / NT;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) hist[NT * x + tid] = 0;
     __syncthreads();
     int bin = 0;
-    for (int i = tid; i < count; i += kPlanThreads) {
+    for (int i = tid; i < count; i += NT) {
       bin = kBuckets - 1 - min(entry(i), kBuckets - 1);
       atomicAdd(&hist[bin], 1);
     }
     __syncthreads();
-    int v[1] = {hist[tid]}, unused[1];
-    scan_all<1>(v, unused, scan_tmp);
-    hist[tid] = v[0];
+    int own[PER], v[1] = {0}, unused[1];
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      own[x] = hist[PER * tid + x];
+      v[0] += own[x];
+    }
+    scan_all<1, NT>(v, unused, scan_tmp);
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      hist[PER * tid + x] = v[0];
+      v[0] += own[x];
+    }
     __syncthreads();
-    for (int i = tid; i < count; i += kPlanThreads) {
-      if (count > kPlanThreads) bin = kBuckets - 1 - min(entry(i), kBuckets - 1);
+    for (int i = tid; i < count; i += NT) {
+      if (count > NT) bin = kBuckets - 1 - min(entry(i), kBuckets - 1);
       store(atomicAdd(&hist[bin], 1));
     }
     __syncthreads();
@@ -1689,7 +1704,8 @@ lethe_status launch_few(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
 template <typename T, int D, bool kCap, int R>
 lethe_status launch_form(const PagedAttnArgs& a, const Sizes& z, hipStream_t s) {
   if (z.max_q <= kFewCols / a.G) return launch_few<T, D, kCap, R>(a, z, s);
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, z.tile);
+  constexpr int plan_threads = R == 16 ? 1024 : 256;
+  hipLaunchKernelGGL(plan_kernel<plan_threads>, dim3(1), dim3(plan_threads), 0, s, a, z.tile);
   if (hipGetLastError() != hipSuccess) return LETHE_ERR_HIP;
   hipLaunchKernelGGL((tile_kernel<T, D, kCap>), dim3((unsigned)(z.items * a.c.HK)), dim3(kTileThreads), 0, s, a, z.tile,
                      z.dec);

@@ -134,6 +134,14 @@ def test_few_queries_over_long_rows():
     run([20000], [2], 4, 1, 64, "f16", 64, 0.9, cap=20.0, seed=6)
 
 
+@pytest.mark.parametrize("B", [70, 300])
+def test_chunks_of_many_sequences(B):
+    """Lists that no longer fit one entry a thread, and the planning block's larger forms."""
+    lens = [1 + 37 * i % 90 for i in range(B)]
+    q_lens = [min(n, 9 + i % 23) if i % 4 else i % 3 for i, n in enumerate(lens)]
+    run(lens, [min(n, q) for n, q in zip(lens, q_lens)], 6, 2, 64, "bf16", 16, 0.9, seed=9)
+
+
 def test_as_many_key_ranges_as_a_tile_can_have():
     run([20000], [6], 4, 1, 64, "f16", 64, 0.9, cap=20.0, seed=7)
     run([4700, 2100, 300], [40, 9, 6], 4, 1, 128, "bf16", 16, 1.0, seed=8)
