@@ -439,14 +439,14 @@ __device__ inline void decode_chunk(const PagedAttnArgs& a, const DecWs& ws, con
         o[nt] = M::mma16(av, p, o[nt]);
       }
       if (apart) {
-        float pw[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) pw[j] = (float)p[j];
 #pragma unroll 1
         while (apart) {
           const int r = (int)__builtin_ctz(apart);
           apart &= apart - 1;
-          const float pr = __shfl(pw[4 * (r >> 4) + (r & 3)], 16 * ((r >> 2) & 3) + s);
+          float mine = 0.0f;  // an index would put p in scratch memory
+#pragma unroll
+          for (int j = 0; j < 8; ++j) mine = j == 4 * (r >> 4) + (r & 3) ? (float)p[j] : mine;
+          const float pr = __shfl(mine, 16 * ((r >> 2) & 3) + s);
           if (base + r <= lim) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -1222,28 +1222,35 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2)
     typename M::x8 p[4];
 #pragma unroll
     for (int mm = 0; mm < 4; ++mm) {
+      const unsigned zg = (unsigned)(z >> (16 * mm)) & 0xffffu;
+      p[mm] = mma_zero<T>();
+      if (zg == 0xffffu && apart == 0) continue;  // no row of these counts
       p[mm] = weights(sa, mm);
-      const unsigned zl = (unsigned)(z >> (16 * mm + 4 * hh));
+      if (zg == 0) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        typename M::x8 av = v_operand(vcur, mm, nt);
+        for (int nt = 0; nt < NT; ++nt) o[nt] = M::mma32(v_operand(vcur, mm, nt), p[mm], o[nt]);
+      } else {
+        const unsigned zl = zg >> (4 * hh);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if ((zl >> (8 * (j >> 2) + (j & 3))) & 1u) av[j] = (T)0.0f;
-        o[nt] = M::mma32(av, p[mm], o[nt]);
+        for (int nt = 0; nt < NT; ++nt) {
+          typename M::x8 av = v_operand(vcur, mm, nt);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if ((zl >> (8 * (j >> 2) + (j & 3))) & 1u) av[j] = (T)0.0f;
+          o[nt] = M::mma32(av, p[mm], o[nt]);
+        }
       }
     }
     l += psum[0] + psum[1];
     if (apart) {
       // Their contributions one by one, to the columns that attend them.
-      float pw[32];
-#pragma unroll
-      for (int x = 0; x < 32; ++x) pw[x] = (float)p[x >> 3][x & 7];
 #pragma unroll 1
       while (apart) {
         const int r = (int)__builtin_ctzll(apart);
         apart &= apart - 1;
-        const float mine = pw[8 * (r >> 4) + 4 * ((r >> 3) & 1) + (r & 3)];
+        float mine = 0.0f;  // an index would put p in scratch memory
+#pragma unroll
+        for (int x = 0; x < 32; ++x) mine = x == 8 * (r >> 4) + 4 * ((r >> 3) & 1) + (r & 3) ? (float)p[x >> 3][x & 7] : mine;
         const float other = __shfl_xor(mine, 32);
         const float pr = ((r >> 2) & 1) == hh ? mine : other;
         if (pos >= ks + st * STEP + r) {
