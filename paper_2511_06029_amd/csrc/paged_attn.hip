@@ -615,9 +615,12 @@ struct PlanHead {
   int items, splits, seeds;  // entries of the lists
   int wide;                  // seed blocks of kSeedWide keys instead of kSeedNarrow
 };
-// Keys of a seeding block; below this many wide ones the narrow ones are used.
-constexpr int kSeedWide = 256, kSeedNarrow = 64, kSeedFill = 512;
-constexpr int kSeedGrid = 1024;  // seeding blocks launched, at most
+// Keys of a seeding block; below this many wide ones, one a CU, the narrow ones
+// are used (2048 queries over 8192 rows, 256 wide blocks: 427 us, 469 narrow; two
+// prompts of 250 to 500 queries beside 30 decoding users, 130: 122 narrow, 134
+// wide).
+constexpr int kSeedWide = 256, kSeedNarrow = 64, kSeedFill = 256;
+constexpr int kSeedGrid = 2048;  // seeding blocks launched, at most
 // One tile and key range, or (splits) one tile with several ranges, or one
 // chunk of a sequence with few columns.  An entry has its sequence's sizes, so
 // that the block that takes it waits for one read before those of its rows.
@@ -1435,9 +1438,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(PagedAttnArgs a, TileWs 
 // instructions: a weight takes a multiply-add, an exp2 and a multiply-add
 // against 8 matrix-core cycles a lane, so the rest is kept small (64 keys a
 // wave share a tile's reads, addresses move by constants) and the products of
-// the next tile run among the weights of this one.  Where the blocks of 256
-// keys do not fill the chip, 64 keys and four groups.
-constexpr int kSeedThreads = 512;
+// the next tile run among the weights of this one.  Blocks of four waves, two a
+// CU, so that one's beginning runs beside the other's weights (109 sequences of
+// 44 to 59 queries over 1428 to 4873 rows, D 64, three rounds a block: 244 us, 304
+// with one block of eight waves; 16 queries over 60000 rows 108, 136).  Where the
+// blocks of 256 keys do not fill the chip, 64 keys and two groups.
+constexpr int kSeedThreads = 256;
 
 template <typename T, int D, bool kCap, int NS, int KW, int IG>
 __device__ inline void seed_block(const PagedAttnArgs& a, const TileWs& ws, const PlanSeed& sq, int h, int kblk0, char* const buf0,
@@ -1609,18 +1615,18 @@ __device__ inline void seed_block(const PagedAttnArgs& a, const TileWs& ws, cons
 template <typename T, int D, bool kCap>
 __global__ __launch_bounds__(kSeedThreads) __attribute__((amdgpu_waves_per_eu(2))) void seed_kernel(PagedAttnArgs a, TileWs ws) {
   constexpr int QTILE = 32 * TileCfg<D>::ROWB;
-  __shared__ __attribute__((aligned(16))) char buf0[4 * QTILE];
-  __shared__ __attribute__((aligned(16))) char buf1[4 * QTILE];
-  __shared__ float sums[2 * kSeedWide];
-  static_assert(2 * kSeedWide >= 4 * kSeedNarrow, "both forms' sums fit");
+  __shared__ __attribute__((aligned(16))) char buf0[2 * QTILE];
+  __shared__ __attribute__((aligned(16))) char buf1[2 * QTILE];
+  __shared__ float sums[kSeedWide];
+  static_assert(kSeedWide >= 2 * kSeedNarrow, "both forms' sums fit");
   const PlanHead head = *ws.head;
   for (int i = blockIdx.x; i < head.seeds * a.c.HK; i += gridDim.x) {
     const PlanSeed x = ws.seeds[i / a.c.HK];
     const int h = i % a.c.HK;
     if (head.wide)
-      seed_block<T, D, kCap, 2, 4, 2>(a, ws, x, h, x.block * kSeedWide, buf0, buf1, sums);
+      seed_block<T, D, kCap, 2, 4, 1>(a, ws, x, h, x.block * kSeedWide, buf0, buf1, sums);
     else
-      seed_block<T, D, kCap, 1, 2, 4>(a, ws, x, h, x.block * kSeedNarrow, buf0, buf1, sums);
+      seed_block<T, D, kCap, 1, 2, 2>(a, ws, x, h, x.block * kSeedNarrow, buf0, buf1, sums);
     __syncthreads();  // the buffers are free
   }
 }
