@@ -24,7 +24,7 @@
 //  3. join_kernel: where a tile's keys were cut.
 //  4. seed_kernel (with scores): key-major second pass, the columns' final
 //     max and sum at hand, in a fixed order without atomics.
-//  Eight prompts of 2048 rows, 32 query heads: 9 + 365 + 5 + 205 us, the tiles
+//  Eight prompts of 2048 rows, 32 query heads: 9 + 366 + 5 + 217 us, the tiles
 //  at 0.76 PFLOP/s; over 32768 rows 1.04 (0.86 capped; a large library product
 //  reaches 1.2).
 #include <algorithm>
